@@ -366,6 +366,95 @@ int32_t ckks_attention(ckks_ctx *ctx, const ckks_attn_desc *desc, const ckks_sof
                        void *ws, size_t ws_bytes, void *stream);
 size_t ckks_attention_workspace_bytes(const ckks_ctx *ctx, const ckks_attn_desc *desc, const ckks_softmax_desc *sm, uint32_t level, uint32_t dim);
 
+/* ---- Masks of score rows, differences of score maps (a decoder's causal mask and the tokens behind a sequence's end; a second score map
+ * subtracted with a learned weight per head) -- both multiply by plaintexts encoded at the scale of the level's last prime and rescale, so
+ * that the scale stays and one limb goes.
+ *   ckks_attention_mask: out[g] = rescale(in[g] * M_g) for the `groups` ciphertexts of a score map.  M_g is 1 where query token i, at position
+ *     i + query_offset, sees the slot's key token j: key_begin <= j < key_end, j <= i + query_offset if causal, j > i + query_offset - window
+ *     if window > 0; else 0.  Key tokens are those ckks_attention_scores pairs with the slot.  Used on exponentials: a masked slot then adds
+ *     nothing to its row's sum, and a row that sees no token comes out as zeros.  key_begin = key_end masks everything.
+ *   ckks_attention_difference: out[g] = a[g] - rescale(b[g] * W), W the weight of the slot's head (weights: device, `heads` doubles, read when
+ *     the kernels run), a[g] without its last limb.  a and b at one level, scales within 2^-30; the result has a's scale.
+ *   ckks_softmax_rows_masked: ckks_softmax_rows with u_g = rescale(p_exp(S_g - shift) * M_g) before the first round: one level more.
+ *     Masked scores have to stay in p_exp's interval like all others (an encrypted value cannot be replaced), and a row's sum may be
+ *     as small as one exponential, or zero in rows without a token, which the inverse square root's polynomials have to stay finite on.
+ *     Workspace: ckks_softmax_rows_workspace_bytes.
+ *   ckks_attention_masked: ckks_attention with that Softmax.
+ *   ckks_attention_differential: the values under softmax(q1 k1) - W softmax(q2 k2), both maps masked if mask is not null: the two maps' scores
+ *     and Softmax, ckks_attention_difference, ckks_attention_values.  All operands at one level; the two maps' score scales within 2^-30.
+ *     Levels: one more than ckks_attention (two with a mask).
+ * Results may not lie on inputs or on each other (ckks_attention_masked and _differential: as ckks_attention).  These calls check and plan
+ * everything before the first launch.  Errors: ARG (key_begin > key_end, key_end > tokens, |query_offset| > 2^31, overlaps), LEVEL, SCALE,
+ * NO_KEY, WORKSPACE, UNSUPPORTED, RANGE as above. */
+typedef struct { uint32_t causal, key_begin, key_end, window; int64_t query_offset; } ckks_attn_mask;
+int32_t ckks_attention_mask(ckks_ctx *ctx, const ckks_attn_desc *desc, const ckks_attn_mask *mask, const ckks_ct *in, ckks_ct *out, void *ws,
+                            size_t ws_bytes, void *stream);
+size_t ckks_attention_mask_workspace_bytes(const ckks_ctx *ctx, const ckks_attn_desc *desc, uint32_t level);
+int32_t ckks_attention_difference(ckks_ctx *ctx, const ckks_attn_desc *desc, const ckks_ct *a, const ckks_ct *b, const double *weights, ckks_ct *out,
+                                  void *ws, size_t ws_bytes, void *stream);
+size_t ckks_attention_difference_workspace_bytes(const ckks_ctx *ctx, const ckks_attn_desc *desc, uint32_t level);
+int32_t ckks_softmax_rows_masked(ckks_ctx *ctx, const ckks_attn_desc *desc, const ckks_softmax_desc *sm, const ckks_attn_mask *mask, const ckks_ct *in,
+                                 const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream);
+int32_t ckks_attention_masked(ckks_ctx *ctx, const ckks_attn_desc *desc, const ckks_softmax_desc *sm, const ckks_attn_mask *mask, const ckks_ct *q,
+                              const ckks_ct *k, uint32_t dim, const ckks_ct *v, uint32_t dim_v, const ckks_evk *rlk, const ckks_evk *keys,
+                              uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream);
+size_t ckks_attention_masked_workspace_bytes(const ckks_ctx *ctx, const ckks_attn_desc *desc, const ckks_softmax_desc *sm, uint32_t level, uint32_t dim);
+int32_t ckks_attention_differential(ckks_ctx *ctx, const ckks_attn_desc *desc, const ckks_softmax_desc *sm, const ckks_attn_mask *mask,
+                                    const double *weights, const ckks_ct *q1, const ckks_ct *k1, const ckks_ct *q2, const ckks_ct *k2, uint32_t dim,
+                                    const ckks_ct *v, uint32_t dim_v, const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws,
+                                    size_t ws_bytes, void *stream);
+size_t ckks_attention_differential_workspace_bytes(const ckks_ctx *ctx, const ckks_attn_desc *desc, const ckks_softmax_desc *sm, uint32_t level, uint32_t dim);
+
+/* ---- Positions and the cache of keys and values (Section 3's call order has the position rotation between the projections and the attention
+ * products, and leaves it undefined) -- on token-shard ciphertexts, the layout the projections write and ckks_attention_pack reads:
+ *     slot = ((copy * dim + d) * heads + h) * token_inner + t,
+ * channel d of head h and token t, features in channel-major order, copy < n / (dim * heads * token_inner) (the copies hold the same values).
+ *   ckks_rotary_table: cos, sin (device, [count][rot_dim / 2] fp64) of the angle of positions first .. first + count - 1, times `magnitude`
+ *     (0: 1).  Pair j turns by theta^(-2 j / rot_dim) per position, for longer contexts than the trained one scaled by kind:
+ *       PLAIN: not;  LINEAR: divided by factor;  BASE: theta is multiplied by factor^(rot_dim / (rot_dim - 2));
+ *       BANDS: by how often the pair turns within original_length: at least turns_many (0: 4) times unchanged, at most turns_few (0: 1) times
+ *              divided by factor, between them blended linearly in the number of turns;
+ *       RAMP:  the same blended linearly in j, from the (rounded down) pair that turns turns_many (0: 32) times to the (rounded up) one that
+ *              turns turns_few (0: 1) times.
+ *     Angles are formed and reduced as sums of two doubles: far positions are as exact as near ones (up to 2^50).  rot_dim even, <= 256.
+ *   ckks_rotary: the position rotation of n shard ciphertexts, slot t of in[i] at row rows[i] + t * row_step of the tables (row_step 0: all slots
+ *     hold one token's copies).  The first rot_dim channels of every head are rotated in pairs: layout HALF pairs d with d + rot_dim / 2,
+ *     INTERLEAVED 2 j with 2 j + 1; channel d of pair j:
+ *         first of the pair: x_d cos_j - x_partner sin_j,      second: x_d cos_j + x_partner sin_j;      other channels stay.
+ *     out = rescale( C x + sum_r S_r rot_r(x) ) for the rotations ckks_rotary_rotations lists (by the distance of the pairs to the left and to
+ *     the right, or one where that is half of dim), C and S_r encoded at the scale of the level's last prime, the products by S_r taken in
+ *     the key-switching basis before the one division by P:
+ *         U = sum_r S_r <ModUp(c1) read through sigma_r, key_r>,   A = (C c0 + sum_r S_r sigma_r(c0), C c1),   out = rescale(ModDown(U) + A).
+ *     out: level - 1, the input's scale.  Ciphertexts of a call with equal rows (queries and keys of a shard) share their plaintexts.
+ *   ckks_cache_append: n shard ciphertexts of new tokens into a cache of pages, a page being the shard ciphertext of token_inner neighbouring
+ *     positions (a fresh one: all residues 0).  Item i fills slots spans[i].begin <= t < spans[i].end of page pages[i] from the same slots of its
+ *     inputs (a token copied to all slots can go anywhere); these slots of the page have to be empty (hold 0), all other slots keep their values:
+ *         keys:    out_k[page] = page_k[page] + ckks_rotary's result with C and S_r zero outside the span, slot t at row
+ *                  spans[i].row + (t - begin) * row_step of the tables;
+ *         values:  out_v[page] = page_v[page] + rescale(v * mask of the span), or + v without its upper limbs where the span is the whole page.
+ *     in_k or in_v may be null (only the other side is appended); cos = sin = null: keys are appended as values are.  page_k, page_v, out_k, out_v:
+ *     host arrays of npages descriptors, of which the named pages are read and written, out_k[p] may be page_k[p] (in place).  Pages at one level l,
+ *     inputs at one level above it per side, of which l + 1 limbs are read; the scales of inputs and pages agree within 2^-30.  A page may be named
+ *     once.  Keys and values of a page written by ckks_cache_append go to ckks_attention_pack as they are, with ckks_attn_mask's key_end at
+ *     the number of tokens.
+ * Written buffers may not overlap each other or anything that is read, but for a page in place.  Errors: ARG (also a table row past table_rows, a
+ * page number past npages, an empty span), LEVEL, SCALE, NO_KEY, WORKSPACE, UNSUPPORTED (dim * heads * token_inner does not divide n, rot_dim odd or
+ * above dim).  Tables are read when the kernels run; values beyond the encoder's range set ckks_encode_range_flag. */
+enum { CKKS_ROTARY_HALF = 0, CKKS_ROTARY_INTERLEAVED = 1 };
+enum { CKKS_ROTARY_PLAIN = 0, CKKS_ROTARY_LINEAR = 1, CKKS_ROTARY_BASE = 2, CKKS_ROTARY_BANDS = 3, CKKS_ROTARY_RAMP = 4 };
+typedef struct { int32_t kind; uint32_t rot_dim; double theta, factor, original_length, turns_few, turns_many, magnitude; } ckks_rotary_scaling;
+typedef struct { uint32_t dim, heads, token_inner, rot_dim, layout, row_step; } ckks_rotary_desc;
+typedef struct { uint32_t begin, end, row; } ckks_cache_span;
+int32_t ckks_rotary_table(ckks_ctx *ctx, const ckks_rotary_scaling *scaling, uint64_t first, uint64_t count, double *cos, double *sin, void *stream);
+int32_t ckks_rotary_rotations(const ckks_ctx *ctx, const ckks_rotary_desc *desc, int64_t *rots, uint32_t cap);
+int32_t ckks_rotary(ckks_ctx *ctx, const ckks_rotary_desc *desc, const ckks_ct *in, const uint32_t *rows, uint32_t n, const double *cos, const double *sin,
+                    uint32_t table_rows, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream);
+size_t ckks_rotary_workspace_bytes(const ckks_ctx *ctx, const ckks_rotary_desc *desc, uint32_t level, uint32_t n);
+int32_t ckks_cache_append(ckks_ctx *ctx, const ckks_rotary_desc *desc, const ckks_ct *in_k, const ckks_ct *in_v, uint32_t n, const uint32_t *pages,
+                          const ckks_cache_span *spans, const ckks_ct *page_k, const ckks_ct *page_v, uint32_t npages, const double *cos, const double *sin,
+                          uint32_t table_rows, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out_k, ckks_ct *out_v, void *ws, size_t ws_bytes, void *stream);
+size_t ckks_cache_append_workspace_bytes(const ckks_ctx *ctx, const ckks_rotary_desc *desc, uint32_t page_level, uint32_t n);
+
 /* Conversion between the projections' token-shard layout and the attention operands (Section 6.2 names an adaptation of
  * the Q/K/V inputs before the attention products and a conversion after them; neither is defined in the text).  Needs
  * diag_block * tokens * heads = n and token_inner = the shards' tokens per ciphertext.  A shard ciphertext c < P holds, in

@@ -474,14 +474,15 @@ class Oracle:
             s = self.add(s, self.rotate(s, keys[ge], ge))
         return s
 
-    def softmax_rows(self, desc: AttnDesc, S, scale: float, shift: float, rounds: int, exp_coeffs, rsqrt_coeffs, rlk, keys: dict):
+    def softmax_rows(self, desc: AttnDesc, S, scale: float, shift: float, rounds: int, exp_coeffs, rsqrt_coeffs, rlk, keys: dict, mask: dict = None):
         """Softmax by doubling with a public shift (Algorithm 1) on score rows spread over several ciphertexts: the row of
         (i, h) consists of the slots (e, i, h), e < diag_block, of every S_g.  Order of steps:
           u_g = poly_eval_tree(S_g + round(-shift * scale), exp_coeffs) for every g;
           per round: t = rescale(mul_relin_sum_g(u_g, u_g)); t = t + rotate(t, r) for the ladder rotations r in ascending
                      order (the row sum, in every slot of the row); lam = poly_eval_tree(t, rsqrt_coeffs[j]);
                      for every g: v = rescale(mul_relin(lam, u_g truncated to lam's level)); u_g = rescale(mul_relin(v, v)).
-        The row sums and the inverse square root are formed once for all groups.  Returns ([groups][2][l][N], scale)."""
+        The row sums and the inverse square root are formed once for all groups.  mask (arguments of mask_slots): u =
+        attention_mask(u) before the first round.  Returns ([groups][2][l][N], scale)."""
         S = _u64(S)
         G = S.shape[0]
         u, su = [], None
@@ -489,6 +490,8 @@ class Oracle:
             z = self.add_const(S[g], int(np.rint(-shift * scale)))
             ug, su = self.poly_eval_tree(z, scale, exp_coeffs, rlk)
             u.append(ug)
+        if mask is not None:
+            u = list(self.attention_mask(desc, np.stack(u), **mask))
         for j in range(rounds):
             lv = u[0].shape[1]
             U = np.stack(u)
@@ -659,6 +662,159 @@ class Oracle:
         of X[c] holds channel d of token c token_inner + t, head h.  Returns [P][2][level-1][N]."""
         E, P, B, Ti = self._pack_shape(desc)
         return self._move_blocks(desc, O, P, keys)
+
+    # ---- position rotation, cache pages, masks and differences of score maps ----------------------------------------
+    def pointwise_mul(self, a, b, first: int):
+        """Residue-wise product of [nl][N] arrays under the primes first .. first + nl - 1."""
+        a = _u64(a); b = _u64(b); out = np.empty_like(a)
+        lib().orc_pointwise_mul(self._h, _p(a, _u64p), _p(b, _u64p), C.c_uint32(first), C.c_uint32(a.shape[0]), _p(out, _u64p))
+        return out
+
+    def encode_extended(self, z, scale: float, level: int):
+        """encode under the limbs q_0 .. q_{level-1}, p_0 .. p_{K-1}: [level+K][N]."""
+        m = self.encode_coeffs(z, scale)
+        return np.concatenate([self.small_to_limbs(m, 0, level), self.small_to_limbs(m, self.L, self.K)])
+
+    def rotary_rotations(self, dim: int, heads: int, token_inner: int, rot_dim: int, interleaved: bool):
+        """Slot rotations that bring a channel its partner: the partner lies `apart` channels away; where that is half a head, one
+        cyclic rotation serves both channels of a pair."""
+        apart = 1 if interleaved else rot_dim // 2
+        step = heads * token_inner
+        return [apart * step] if 2 * apart == dim else [apart * step, -apart * step]
+
+    def rotary_slots(self, dim: int, heads: int, token_inner: int, rot_dim: int, interleaved: bool, cos, sin, row: int, row_step: int,
+                     begin: int, end: int):
+        """Slot vectors [C, S_r ...] of a shard ciphertext (slot ((copy dim + d) heads + h) token_inner + t): token t of
+        [begin, end) takes row + (t - begin) row_step of the tables, the others zeros.  Channel d < rot_dim of pair j has
+        C = cos, and S of its partner: -sin for the first channel of the pair, sin for the second."""
+        C_ = np.zeros(self.n)
+        rots = self.rotary_rotations(dim, heads, token_inner, rot_dim, interleaved)
+        S = [np.zeros(self.n) for _ in rots]
+        x = np.arange(self.n)
+        t, d = x % token_inner, x // (token_inner * heads) % dim
+        live = (t >= begin) & (t < end)
+        C_[live & (d >= rot_dim)] = 1.0
+        for dd in range(rot_dim):
+            j = dd // 2 if interleaved else dd % (rot_dim // 2)
+            second = dd % 2 == 1 if interleaved else dd >= rot_dim // 2
+            at = live & (d == dd)
+            rows = row + (t[at] - begin) * row_step
+            C_[at] = cos[rows, j]
+            S[-1 if second else 0][at] = sin[rows, j] if second else -sin[rows, j]
+        return [C_] + S
+
+    def rotary_apply(self, ct, slots, rots, keys: dict):
+        """rescale( C ct + sum_r S_r rotate(ct, r) ) with plaintexts at the scale of the level's last prime and the products by
+        S_r taken in the key-switching basis, before one division by P:
+          U = sum_r S_r <ModUp(c1) read through sigma_r, key_r>  (limbs of Q_level P);
+          A = (C c0 + sum_r S_r sigma_r(c0), C c1);  result rescale(ModDown(U) + A)."""
+        ct = _u64(ct); level = ct.shape[1]
+        scale = float(self.q[level - 1])
+        acc = self.mul_plain_acc(ct, self.encode(slots[0], scale, level))
+        ext, U = self.modup_all(ct[1]), None
+        L_, T = self.L, level + self.K
+        for S, r in zip(slots[1:], rots):
+            g = self.galois_element(r)
+            pt = self.encode_extended(S, scale, level)
+            sig = np.stack([np.stack([self.automorphism_eval(e[x], g) for x in range(T)]) for e in ext])
+            u = self.inner_product(sig, keys[g])
+            w = np.stack([np.concatenate([self.pointwise_mul(u[c][:level], pt[:level], 0), self.pointwise_mul(u[c][level:], pt[level:], L_)])
+                          for c in range(2)])
+            U = w if U is None else self._add_extended(U, w, level)
+            c0 = np.stack([self.automorphism_eval(ct[0][x], g) for x in range(level)])
+            acc[0] = self.add(acc[0][None], self.pointwise_mul(c0, pt[:level], 0)[None])[0]
+        k = np.stack([self.moddown(U[c], level) for c in range(2)])
+        return self.rescale(self.add(acc, k))
+
+    def _add_extended(self, a, b, level: int):
+        m = np.array(self.q[:level] + self.p, dtype=np.uint64)[None, :, None]
+        s = a + b
+        return np.where(s >= m, s - m, s)
+
+    def rotary(self, cts, rows, cos, sin, keys: dict, dim: int, heads: int, token_inner: int, rot_dim: int, interleaved: bool, row_step: int = 1):
+        """Position rotation of shard ciphertexts: slot t of cts[i] takes row rows[i] + t row_step of cos, sin [rows][rot_dim / 2]."""
+        rots = self.rotary_rotations(dim, heads, token_inner, rot_dim, interleaved)
+        return np.stack([self.rotary_apply(c, self.rotary_slots(dim, heads, token_inner, rot_dim, interleaved, cos, sin, r, row_step, 0, token_inner),
+                                           rots, keys) for c, r in zip(_u64(cts), rows)])
+
+    def token_mask(self, token_inner: int, begin: int, end: int):
+        t = np.arange(self.n) % token_inner
+        return ((t >= begin) & (t < end)).astype(np.float64)
+
+    def append_values(self, page, v, token_inner: int, begin: int, end: int):
+        """page + the tokens [begin, end) of v: as they are where they fill the page, else rescale(v mask).  page has level l, v at least
+        l + 1, of which l + 1 limbs (l for a full page) are read."""
+        page = _u64(page); v = _u64(v); level = page.shape[1]
+        if begin == 0 and end == token_inner:
+            return self.add(page, v[:, :level])
+        v = np.ascontiguousarray(v[:, :level + 1])
+        mask = self.encode(self.token_mask(token_inner, begin, end), float(self.q[level]), level + 1)
+        return self.add(page, self.rescale(self.mul_plain_acc(v, mask)))
+
+    def append_keys(self, page, k, cos, sin, keys: dict, dim: int, heads: int, token_inner: int, rot_dim: int, interleaved: bool, begin: int,
+                    end: int, row: int):
+        """page + the tokens [begin, end) of k rotated to the positions row, row + 1, .. of the tables."""
+        page = _u64(page); level = page.shape[1]
+        k = np.ascontiguousarray(_u64(k)[:, :level + 1])
+        slots = self.rotary_slots(dim, heads, token_inner, rot_dim, interleaved, cos, sin, row, 1, begin, end)
+        return self.add(page, self.rotary_apply(k, slots, self.rotary_rotations(dim, heads, token_inner, rot_dim, interleaved), keys))
+
+    def attention_masked(self, desc: AttnDesc, q, k, v, scale: float, v_scale: float, shift: float, rounds: int, exp_coeffs, rsqrt_coeffs, rlk, keys: dict,
+                         mask: dict = None, weights=None):
+        """attention with masked rows; q, k pairs of operand sets with weights: the values under the difference of the two maps.
+        Returns ([dim_v][2][l][N], scale)."""
+        maps = []
+        for qm, km in ([(q, k)] if weights is None else zip(q, k)):
+            level = _u64(qm).shape[2]
+            S = self.attention_scores(desc, qm, km, rlk, keys)
+            P, sp = self.softmax_rows(desc, S, scale * scale / float(self.q[level - 1]), shift, rounds, exp_coeffs, rsqrt_coeffs, rlk, keys, mask)
+            maps.append(P)
+        P = maps[0] if weights is None else self.attention_difference(desc, maps[0], maps[1], weights)
+        return self.attention_values(desc, P, v, rlk, keys), sp * v_scale / float(self.q[P.shape[2] - 1])
+
+    def score_places(self, desc: AttnDesc):
+        """(block e, query token i, head h) of every slot of a score ciphertext."""
+        Ti, H, per = desc.token_inner, desc.heads, desc.tokens // desc.token_inner
+        x = np.arange(self.n) // (self.n // (desc.diag_block * desc.tokens * H))
+        t, h, pos = x % Ti, x // Ti % H, x // (Ti * H)
+        return pos // per, pos % per * Ti + t, h
+
+    def score_keys(self, desc: AttnDesc, g: int):
+        """Key token of every slot of S_g: that of the key operand (token i + e in block e) rotated left by g diag_block tokens over
+        the flattened (e, i) index."""
+        e, i, _ = self.score_places(desc)
+        flat = (e * desc.tokens + i + g * desc.diag_block) % (desc.diag_block * desc.tokens)
+        return (flat % desc.tokens + flat // desc.tokens) % desc.tokens
+
+    def mask_slots(self, desc: AttnDesc, g: int, causal: bool, key_begin: int, key_end: int, window: int = 0, query_offset: int = 0):
+        """1.0 where query i (at position i + query_offset) sees key token j: key_begin <= j < key_end, j <= i + query_offset where causal,
+        j > i + query_offset - window where window > 0."""
+        _, i, _ = self.score_places(desc)
+        j, at = self.score_keys(desc, g), i + query_offset
+        live = (j >= key_begin) & (j < key_end)
+        if causal:
+            live &= j <= at
+        if window:
+            live &= j > at - window
+        return live.astype(np.float64)
+
+    def attention_mask(self, desc: AttnDesc, X, **mask):
+        """rescale(X_g M_g) for every group g, M_g encoded at the scale of the level's last prime."""
+        X = _u64(X); level = X.shape[2]
+        return np.stack([self.rescale(self.mul_plain_acc(x, self.encode(self.mask_slots(desc, g, **mask), float(self.q[level - 1]), level)))
+                         for g, x in enumerate(X)])
+
+    def attention_difference(self, desc: AttnDesc, X, Y, weights):
+        """X_g without its last limb minus rescale(Y_g W), W the weight of a slot's head at the scale of the level's last prime."""
+        X = _u64(X); Y = _u64(Y); level = X.shape[2]
+        _, _, h = self.score_places(desc)
+        pt = self.encode(np.asarray(weights, dtype=np.float64)[h], float(self.q[level - 1]), level)
+        m = np.array(self.q[:level - 1], dtype=np.uint64)[None, :, None]
+        out = []
+        for x, y in zip(X, Y):
+            w, x = self.rescale(self.mul_plain_acc(y, pt)), x[:, :level - 1]
+            out.append(np.where(x >= w, x - w, x + m - w))
+        return np.stack(out)
 
     def automorphism_coeff(self, a, g: int, t: int):
         a = _u64(a); out = np.empty_like(a)

@@ -20,6 +20,8 @@ OPT_NTT_FP_SHARE, OPT_CONV_KERNEL, OPT_MAC_KERNEL, OPT_WAIT_CYCLES, OPT_STATIC_S
 CONV_FP64, CONV_TENSOR = 0, 1
 MAC_MMA, MAC_MMA_ASYNC, MAC_MMA_SPLIT, MAC_MMA_HALF, MAC_TCGEN05 = 82, 83, 81, 42, 100
 ATTN_QUERY, ATTN_KEY_VALUE, ATTN_TO_SHARDS = 0, 1, 2
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
 
 EXPORTS = [
     "ckks_context_create", "ckks_context_destroy", "ckks_context_set_option", "ckks_context_get_option", "ckks_status_string",
@@ -31,6 +33,10 @@ EXPORTS = [
     "ckks_poly_eval_bsgs_batch", "ckks_poly_eval_bsgs_batch_workspace_bytes", "ckks_attention_pack_rotations", "ckks_attention_pack", "ckks_attention_pack_workspace_bytes", "ckks_attention_rotations", "ckks_attention_scores", "ckks_attention_scores_workspace_bytes", "ckks_attention_values",
     "ckks_attention_values_workspace_bytes", "ckks_softmax_rows", "ckks_softmax_rows_workspace_bytes", "ckks_attention",
     "ckks_attention_workspace_bytes",
+    "ckks_attention_mask", "ckks_attention_mask_workspace_bytes", "ckks_attention_difference", "ckks_attention_difference_workspace_bytes",
+    "ckks_softmax_rows_masked", "ckks_attention_masked", "ckks_attention_masked_workspace_bytes", "ckks_attention_differential",
+    "ckks_attention_differential_workspace_bytes", "ckks_rotary_table", "ckks_rotary_rotations", "ckks_rotary", "ckks_rotary_workspace_bytes",
+    "ckks_cache_append", "ckks_cache_append_workspace_bytes",
     "ckks_ntt_butterfly_probe", "ckks_mul_relin_sum", "ckks_mul_relin_batch", "ckks_rotate_batch", "ckks_rotate_sum", "ckks_softmax", "ckks_softmax_workspace_bytes", "ckks_poly_eval_bsgs", "ckks_poly_eval_bsgs_workspace_bytes", "ckks_mul_const", "ckks_add_const", "ckks_poly_eval", "ckks_poly_eval_tree", "ckks_linear_proj_multi", "ckks_linear_proj_multi_workspace_bytes",
 ]
 
@@ -60,6 +66,24 @@ class CSoftmaxDesc(C.Structure):
 
 class CAttnDesc(C.Structure):
     _fields_ = [("tokens", C.c_uint32), ("heads", C.c_uint32), ("diag_block", C.c_uint32), ("group_baby", C.c_uint32), ("token_inner", C.c_uint32)]
+
+
+class CAttnMask(C.Structure):
+    _fields_ = [("causal", C.c_uint32), ("key_begin", C.c_uint32), ("key_end", C.c_uint32), ("window", C.c_uint32), ("query_offset", C.c_int64)]
+
+
+class CRotaryScaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("rot_dim", C.c_uint32), ("theta", C.c_double), ("factor", C.c_double), ("original_length", C.c_double),
+                ("turns_few", C.c_double), ("turns_many", C.c_double), ("magnitude", C.c_double)]
+
+
+class CRotaryDesc(C.Structure):
+    _fields_ = [("dim", C.c_uint32), ("heads", C.c_uint32), ("token_inner", C.c_uint32), ("rot_dim", C.c_uint32), ("layout", C.c_uint32),
+                ("row_step", C.c_uint32)]
+
+
+class CCacheSpan(C.Structure):
+    _fields_ = [("begin", C.c_uint32), ("end", C.c_uint32), ("row", C.c_uint32)]
 
 
 class CProjDesc(C.Structure):
@@ -119,6 +143,26 @@ def load():
         "ckks_attention": (i32, [vp, C.POINTER(CAttnDesc), C.POINTER(CSoftmaxDesc), C.POINTER(CCt), C.POINTER(CCt), u32, C.POINTER(CCt), u32,
                                  C.POINTER(CEvk), C.POINTER(CEvk), u32, C.POINTER(CCt), vp, sz, vp]),
         "ckks_attention_workspace_bytes": (sz, [vp, C.POINTER(CAttnDesc), C.POINTER(CSoftmaxDesc), u32, u32]),
+        "ckks_attention_mask": (i32, [vp, C.POINTER(CAttnDesc), C.POINTER(CAttnMask), C.POINTER(CCt), C.POINTER(CCt), vp, sz, vp]),
+        "ckks_attention_mask_workspace_bytes": (sz, [vp, C.POINTER(CAttnDesc), u32]),
+        "ckks_attention_difference": (i32, [vp, C.POINTER(CAttnDesc), C.POINTER(CCt), C.POINTER(CCt), vp, C.POINTER(CCt), vp, sz, vp]),
+        "ckks_attention_difference_workspace_bytes": (sz, [vp, C.POINTER(CAttnDesc), u32]),
+        "ckks_softmax_rows_masked": (i32, [vp, C.POINTER(CAttnDesc), C.POINTER(CSoftmaxDesc), C.POINTER(CAttnMask), C.POINTER(CCt), C.POINTER(CEvk),
+                                           C.POINTER(CEvk), u32, C.POINTER(CCt), vp, sz, vp]),
+        "ckks_attention_masked": (i32, [vp, C.POINTER(CAttnDesc), C.POINTER(CSoftmaxDesc), C.POINTER(CAttnMask), C.POINTER(CCt), C.POINTER(CCt), u32,
+                                        C.POINTER(CCt), u32, C.POINTER(CEvk), C.POINTER(CEvk), u32, C.POINTER(CCt), vp, sz, vp]),
+        "ckks_attention_masked_workspace_bytes": (sz, [vp, C.POINTER(CAttnDesc), C.POINTER(CSoftmaxDesc), u32, u32]),
+        "ckks_attention_differential": (i32, [vp, C.POINTER(CAttnDesc), C.POINTER(CSoftmaxDesc), C.POINTER(CAttnMask), vp, C.POINTER(CCt), C.POINTER(CCt),
+                                              C.POINTER(CCt), C.POINTER(CCt), u32, C.POINTER(CCt), u32, C.POINTER(CEvk), C.POINTER(CEvk), u32,
+                                              C.POINTER(CCt), vp, sz, vp]),
+        "ckks_attention_differential_workspace_bytes": (sz, [vp, C.POINTER(CAttnDesc), C.POINTER(CSoftmaxDesc), u32, u32]),
+        "ckks_rotary_table": (i32, [vp, C.POINTER(CRotaryScaling), u64, u64, vp, vp, vp]),
+        "ckks_rotary_rotations": (i32, [vp, C.POINTER(CRotaryDesc), C.POINTER(i64), u32]),
+        "ckks_rotary": (i32, [vp, C.POINTER(CRotaryDesc), C.POINTER(CCt), C.POINTER(u32), u32, vp, vp, u32, C.POINTER(CEvk), u32, C.POINTER(CCt), vp, sz, vp]),
+        "ckks_rotary_workspace_bytes": (sz, [vp, C.POINTER(CRotaryDesc), u32, u32]),
+        "ckks_cache_append": (i32, [vp, C.POINTER(CRotaryDesc), C.POINTER(CCt), C.POINTER(CCt), u32, C.POINTER(u32), C.POINTER(CCacheSpan), C.POINTER(CCt),
+                                    C.POINTER(CCt), u32, vp, vp, u32, C.POINTER(CEvk), u32, C.POINTER(CCt), C.POINTER(CCt), vp, sz, vp]),
+        "ckks_cache_append_workspace_bytes": (sz, [vp, C.POINTER(CRotaryDesc), u32, u32]),
         "ckks_rotate_sum": (i32, [vp, C.POINTER(CCt), C.POINTER(CEvk), u32, C.POINTER(CCt), vp, sz, vp]),
         "ckks_rotate_batch": (i32, [vp, C.POINTER(CCt), u32, C.POINTER(CEvk), C.POINTER(CCt), vp, sz, vp]),
         "ckks_mul_relin_batch": (i32, [vp, C.POINTER(CCt), C.POINTER(CCt), u32, C.POINTER(CEvk), C.POINTER(CCt), vp, sz, vp]),
@@ -577,6 +621,219 @@ class Context:
         self._check(_lib.ckks_attention(self._h, C.byref(d), C.byref(sd), qa, ka, len(q), va, len(v), C.byref(ck), ra, len(keys), oa,
                                           ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
         return [self._cut(o, c) for o, c in zip(outs, oa)]
+
+    # ------------------------------------------- masks, differences, positions, cache
+    def _evks(self, keys):
+        return (CEvk * max(1, len(keys)))(*[CEvk(_dev_u64(x.data).data_ptr(), x.galois) for x in keys])
+
+    @staticmethod
+    def _mask(tokens, causal, key_begin, key_end, window, query_offset):
+        return CAttnMask(int(bool(causal)), key_begin, tokens if key_end is None else key_end, window, query_offset)
+
+    def _results(self, outs, count, level):
+        """Result ciphertexts at `level`: the caller's (checked) or fresh ones."""
+        if outs is None:
+            return [self.empty_ct(level) for _ in range(count)]
+        if len(outs) != count or any(tuple(o.data.shape) != (2, level, self.N) for o in outs):
+            raise ValueError(f"expected {count} results of shape (2, {level}, {self.N})")
+        return outs
+
+    def _of_ring(self, *lists):
+        """Every ciphertext of the lists has two components and this ring's degree."""
+        for cts in lists:
+            for x in cts:
+                if x.data.dim() != 3 or x.data.shape[0] != 2 or x.data.shape[2] != self.N:
+                    raise ValueError(f"expected ciphertexts of shape (2, level, {self.N})")
+
+    def attention_mask(self, cts, tokens, heads, diag_block, token_inner: int = 1, causal: bool = False, key_begin: int = 0, key_end: int = None,
+                       window: int = 0, query_offset: int = 0, outs=None, ws: torch.Tensor = None, stream=None):
+        """Score-map ciphertexts (one per group) with the slots of unseen key tokens set to 0, one level down: key tokens outside
+        [key_begin, key_end), past the query's position i + query_offset if causal, `window` or more positions before it if window > 0."""
+        d = CAttnDesc(tokens, heads, diag_block, 1, token_inner)
+        m = self._mask(tokens, causal, key_begin, key_end, window, query_offset)
+        if diag_block < 1 or len(cts) != tokens // diag_block:
+            raise ValueError("expected one ciphertext per group of diag_block diagonals")
+        self._of_ring(cts)
+        level = cts[0].level
+        need = int(load().ckks_attention_mask_workspace_bytes(self._h, C.byref(d), level))
+        ws = self.workspace(need) if ws is None else ws
+        outs = self._results(outs, len(cts), max(level - 1, 1))
+        ia, oa = (CCt * len(cts))(*[_cct(x) for x in cts]), (CCt * len(cts))(*[_cct(x) for x in outs])
+        self._check(_lib.ckks_attention_mask(self._h, C.byref(d), C.byref(m), ia, oa, ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
+        for o, c in zip(outs, oa):
+            o.scale = c.scale
+        return outs
+
+    def _weights(self, weights: torch.Tensor, heads: int) -> int:
+        if not (weights.is_cuda and weights.dtype == torch.float64 and weights.is_contiguous() and weights.numel() == heads):
+            raise TypeError("expected a contiguous CUDA float64 tensor of one weight per head")
+        return weights.data_ptr()
+
+    def attention_difference(self, a, b, weights: torch.Tensor, tokens, heads, diag_block, token_inner: int = 1, outs=None, ws: torch.Tensor = None,
+                             stream=None):
+        """a[g] - weights[head] b[g] for the groups of two score maps, one level down.  weights: float64 [heads] on the device."""
+        d = CAttnDesc(tokens, heads, diag_block, 1, token_inner)
+        if diag_block < 1 or len(a) != tokens // diag_block or len(b) != len(a):
+            raise ValueError("expected one ciphertext per group of diag_block diagonals")
+        self._of_ring(a, b)
+        level = a[0].level
+        need = int(load().ckks_attention_difference_workspace_bytes(self._h, C.byref(d), level))
+        ws = self.workspace(need) if ws is None else ws
+        outs = self._results(outs, len(a), max(level - 1, 1))
+        aa, ba, oa = ((CCt * len(a))(*[_cct(x) for x in v]) for v in (a, b, outs))
+        self._check(_lib.ckks_attention_difference(self._h, C.byref(d), aa, ba, self._weights(weights, heads), oa, ws.data_ptr(), ws.numel(),
+                                                   _stream_ptr(stream)))
+        for o, c in zip(outs, oa):
+            o.scale = c.scale
+        return outs
+
+    def softmax_rows_masked(self, cts, shift, rounds, exp_coeffs, rsqrt_coeffs, rlk: SwitchKey, keys, tokens, heads, diag_block, token_inner: int = 1,
+                            causal: bool = False, key_begin: int = 0, key_end: int = None, window: int = 0, query_offset: int = 0, stream=None):
+        """softmax_rows over the key tokens that a query sees (see attention_mask), one level more."""
+        d = CAttnDesc(tokens, heads, diag_block, 1, token_inner)
+        sd = self._softmax_desc(shift, rounds, exp_coeffs, rsqrt_coeffs)
+        m = self._mask(tokens, causal, key_begin, key_end, window, query_offset)
+        if diag_block < 1 or len(cts) != tokens // diag_block:
+            raise ValueError("expected one ciphertext per group of diag_block diagonals")
+        self._of_ring(cts)
+        level = cts[0].level
+        need = int(load().ckks_softmax_rows_workspace_bytes(self._h, C.byref(d), C.byref(sd), level))
+        if need == 0:
+            raise CkksError(ERR_ARG)
+        ws = self.workspace(need)
+        outs = [self.empty_ct(level) for _ in cts]
+        ia, oa = ((CCt * len(cts))(*[_cct(x) for x in v]) for v in (cts, outs))
+        ck = CEvk(_dev_u64(rlk.data).data_ptr(), 0)
+        self._check(_lib.ckks_softmax_rows_masked(self._h, C.byref(d), C.byref(sd), C.byref(m), ia, C.byref(ck), self._evks(keys), len(keys), oa,
+                                                  ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
+        return [self._cut(o, c) for o, c in zip(outs, oa)]
+
+    def attention_masked(self, q, k, v, shift, rounds, exp_coeffs, rsqrt_coeffs, rlk: SwitchKey, keys, tokens, heads, diag_block, token_inner: int = 1,
+                         group_baby: int = 1, causal: bool = False, key_begin: int = 0, key_end: int = None, window: int = 0, query_offset: int = 0,
+                         ws: torch.Tensor = None, stream=None):
+        """attention over the key tokens that a query sees (see attention_mask)."""
+        m = self._mask(tokens, causal, key_begin, key_end, window, query_offset)
+        return self._attend(m, None, [q], [k], v, shift, rounds, exp_coeffs, rsqrt_coeffs, rlk, keys, (tokens, heads, diag_block, group_baby, token_inner),
+                            ws, stream)
+
+    def attention_differential(self, q1, k1, q2, k2, v, weights: torch.Tensor, shift, rounds, exp_coeffs, rsqrt_coeffs, rlk: SwitchKey, keys, tokens,
+                               heads, diag_block, token_inner: int = 1, group_baby: int = 1, masked: bool = False, causal: bool = False,
+                               key_begin: int = 0, key_end: int = None, window: int = 0, query_offset: int = 0, ws: torch.Tensor = None, stream=None):
+        """The values under softmax(q1 k1) - weights[head] softmax(q2 k2); `masked`: both over the key tokens that a query sees."""
+        m = self._mask(tokens, causal, key_begin, key_end, window, query_offset) if masked else None
+        return self._attend(m, weights, [q1, q2], [k1, k2], v, shift, rounds, exp_coeffs, rsqrt_coeffs, rlk, keys,
+                            (tokens, heads, diag_block, group_baby, token_inner), ws, stream)
+
+    def _attend(self, mask, weights, qs, ks, v, shift, rounds, exp_coeffs, rsqrt_coeffs, rlk, keys, shape, ws, stream):
+        d = CAttnDesc(*shape)
+        sd = self._softmax_desc(shift, rounds, exp_coeffs, rsqrt_coeffs)
+        dim, level = len(qs[0]), qs[0][0].level
+        if any(len(x) != dim for x in (*qs, *ks)):
+            raise ValueError("expected one query and one key operand per channel")
+        self._of_ring(*qs, *ks, v)
+        L = load()
+        size = L.ckks_attention_differential_workspace_bytes if weights is not None else L.ckks_attention_masked_workspace_bytes
+        need = int(size(self._h, C.byref(d), C.byref(sd), level, dim))
+        if need == 0:
+            raise CkksError(ERR_ARG)
+        ws = self.workspace(need) if ws is None else ws
+        outs = [self.empty_ct(level - 1) for _ in v]
+        qa, ka = ([(CCt * dim)(*[_cct(x) for x in cts]) for cts in side] for side in (qs, ks))
+        va, oa = ((CCt * len(v))(*[_cct(x) for x in cts]) for cts in (v, outs))
+        ck = CEvk(_dev_u64(rlk.data).data_ptr(), 0)
+        tail = (dim, va, len(v), C.byref(ck), self._evks(keys), len(keys), oa, ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+        if weights is None:
+            self._check(L.ckks_attention_masked(self._h, C.byref(d), C.byref(sd), C.byref(mask), qa[0], ka[0], *tail))
+        else:
+            self._check(L.ckks_attention_differential(self._h, C.byref(d), C.byref(sd), C.byref(mask) if mask is not None else None,
+                                                      self._weights(weights, shape[1]), qa[0], ka[0], qa[1], ka[1], *tail))
+        return [self._cut(o, c) for o, c in zip(outs, oa)]
+
+    def rotary_table(self, rot_dim: int, first: int, count: int, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                     original_length: float = 0.0, turns_few: float = 0.0, turns_many: float = 0.0, magnitude: float = 1.0, out=None, stream=None):
+        """(cos, sin), float64 [count][rot_dim / 2], of the positions first .. first + count - 1."""
+        f = CRotaryScaling(ROTARY_SCALINGS[scaling], rot_dim, theta, factor, original_length, turns_few, turns_many, magnitude)
+        shape = (count, rot_dim // 2)
+        if out is None:
+            out = tuple(torch.empty(shape, dtype=torch.float64, device=self.device) for _ in range(2))
+        for t in out:
+            if not (t.is_cuda and t.dtype == torch.float64 and t.is_contiguous() and tuple(t.shape) == shape):
+                raise TypeError("expected contiguous CUDA float64 tensors [count][rot_dim / 2]")
+        self._check(_lib.ckks_rotary_table(self._h, C.byref(f), first, count, out[0].data_ptr(), out[1].data_ptr(), _stream_ptr(stream)))
+        return out
+
+    @staticmethod
+    def _rotary_desc(dim, heads, token_inner, rot_dim, layout, same_position=False):
+        return CRotaryDesc(dim, heads, token_inner, dim if rot_dim is None else rot_dim, ROTARY_LAYOUTS[layout], 0 if same_position else 1)
+
+    def rotary_rotations(self, dim: int, heads: int, token_inner: int, rot_dim: int = None, layout: str = "half"):
+        """Rotations (in slots, negative: to the right) whose keys rotary and cache_append need."""
+        d = self._rotary_desc(dim, heads, token_inner, rot_dim, layout)
+        n = load().ckks_rotary_rotations(self._h, C.byref(d), None, 0)
+        if n < 0:
+            raise CkksError(n)
+        buf = (C.c_int64 * n)()
+        load().ckks_rotary_rotations(self._h, C.byref(d), buf, n)
+        return list(buf)
+
+    @staticmethod
+    def _table(cos, sin, d):
+        for t in (cos, sin):
+            if not (t.is_cuda and t.dtype == torch.float64 and t.is_contiguous() and t.dim() == 2 and t.shape[1] * 2 == d.rot_dim and t.shape[0] == cos.shape[0]):
+                raise TypeError("expected contiguous CUDA float64 tensors [rows][rot_dim / 2]")
+        return cos.data_ptr(), sin.data_ptr(), cos.shape[0]
+
+    def rotary(self, cts, rows, cos: torch.Tensor, sin: torch.Tensor, keys, dim: int, heads: int, token_inner: int, rot_dim: int = None,
+               layout: str = "half", same_position: bool = False, outs=None, ws: torch.Tensor = None, stream=None):
+        """Position rotation of shard ciphertexts, one level down: slot t of cts[i] takes row rows[i] + t of the tables (rows[i] with
+        same_position, where all slots hold one token)."""
+        d = self._rotary_desc(dim, heads, token_inner, rot_dim, layout, same_position)
+        n, level = len(cts), cts[0].level
+        if len(rows) != n:
+            raise ValueError("expected one table row per ciphertext")
+        self._of_ring(cts)
+        need = int(load().ckks_rotary_workspace_bytes(self._h, C.byref(d), level, n))
+        ws = self.workspace(need) if ws is None else ws
+        outs = self._results(outs, n, max(level - 1, 1))
+        ia, oa = ((CCt * n)(*[_cct(x) for x in v]) for v in (cts, outs))
+        self._check(_lib.ckks_rotary(self._h, C.byref(d), ia, (C.c_uint32 * n)(*rows), n, *self._table(cos, sin, d), self._evks(keys), len(keys), oa,
+                                     ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
+        for o, c in zip(outs, oa):
+            o.scale = c.scale
+        return outs
+
+    def cache_append(self, cts_k, cts_v, pages, spans, page_k, page_v, cos, sin, keys, dim: int, heads: int, token_inner: int, rot_dim: int = None,
+                     layout: str = "half", same_position: bool = False, out_k=None, out_v=None, ws: torch.Tensor = None, stream=None):
+        """New tokens into pages: slots [begin, end) of cts_k[i], rotated to the positions row, row + 1, .. of the tables, and of cts_v[i] are
+        added to page pages[i], spans[i] = (begin, end, row).  In place unless out_k, out_v name other ciphertexts (one per page; those of
+        pages that are not named are left alone).  cts_k or cts_v None: only the other side; cos, sin None: keys without positions."""
+        d = self._rotary_desc(dim, heads, token_inner, rot_dim, layout, same_position)
+        n = len(pages)
+        sides, npages, level = [], None, None
+        for cts, pool, out in ((cts_k, page_k, out_k), (cts_v, page_v, out_v)):
+            if cts is None:
+                sides.append((None, None, None, None))
+                continue
+            out = pool if out is None else out
+            if len(cts) != n or len(spans) != n or len(out) != len(pool) or npages not in (None, len(pool)):
+                raise ValueError("expected one ciphertext and span per page named, and as many results as pages")
+            self._of_ring(cts, pool, out)
+            npages, level = len(pool), pool[0].level
+            if any(0 <= p < npages and out[p].level != level for p in pages):
+                raise ValueError("expected results of the pages' level")
+            sides.append(((CCt * n)(*[_cct(x) for x in cts]), (CCt * npages)(*[_cct(x) for x in pool]), (CCt * npages)(*[_cct(x) for x in out]), out))
+        if npages is None:
+            raise CkksError(ERR_ARG)
+        need = int(load().ckks_cache_append_workspace_bytes(self._h, C.byref(d), level, n))
+        ws = self.workspace(need) if ws is None else ws
+        table = self._table(cos, sin, d) if cos is not None else (None, None, 0)
+        (ik, pk, ok, _), (iv, pv, ov, _) = sides
+        self._check(_lib.ckks_cache_append(self._h, C.byref(d), ik, iv, n, (C.c_uint32 * n)(*pages), (CCacheSpan * n)(*[CCacheSpan(*x) for x in spans]), pk, pv,
+                                           npages, *table, self._evks(keys), len(keys), ok, ov, ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
+        for _, _, oa, out in sides:
+            for p in pages if out is not None else ():
+                out[p].scale = oa[p].scale
+        return (out_k if out_k is not None else page_k), (out_v if out_v is not None else page_v)
 
     def rotate_sum(self, cts, keys, out: Ciphertext = None, ws: torch.Tensor = None, stream=None):
         """sum_i rotate(cts[i], keys[i]) formed in the key-switching basis and divided by P once."""

@@ -1,5 +1,6 @@
 // Attention in the diagonal-block layout on buffers carved from the caller's workspace: the products from the batched steps of
-// batch.cu and poly.cu, the layout conversions from the entry points of api.cu.  No kernels of its own.
+// batch.cu and poly.cu, masks and differences from launch_plain_rescale, the layout conversions from the entry points of api.cu.  No kernels
+// of its own.
 //
 // Layout.  Every operand and every score ciphertext uses the slot index
 //     slot = ((e * tokens + i) * heads + h) * R + r,      R = n / (diag_block * tokens * heads),
@@ -74,6 +75,10 @@ int check_cts(const ckks_ctx *c, const ckks_ct *cts, uint32_t n, uint32_t *level
 
 bool rlk_ok(const ckks_evk *rlk) { return rlk && rlk->data && rlk->galois == 0; }
 
+bool apart(const void *a, size_t na, const void *b, size_t nb) {
+    const char *x = (const char *)a, *y = (const char *)b;
+    return x + na <= y || y + nb <= x;
+}
 
 uint32_t log2_ceil(uint32_t x) { uint32_t d = 0; while ((1u << d) < x) d++; return d; }
 
@@ -207,6 +212,124 @@ extern "C" int32_t ckks_attention_scores(ckks_ctx *c, const ckks_attn_desc *d, c
     return rc;
 }
 
+// ---- masks of score rows, differences of score maps --------------------------------------------------------------------
+// Both are a product with a plaintext and its rescale (launch_plain_rescale): 0/1 where a query sees a key token, or minus the weight of
+// the slot's head, whose product is then added to the other map.
+static bool mask_ok(const AttnPlan &p, const ckks_attn_mask *m) {
+    return m && m->key_begin <= m->key_end && m->key_end <= p.Tk && m->query_offset >= -(1ll << 31) && m->query_offset <= (1ll << 31);
+}
+static size_t plain_steps_bytes(const ckks_ctx *c, uint32_t level, uint32_t n, uint32_t pts) {
+    return align256((size_t)pts * level * c->N * sizeof(u64)) +
+           align256(std::max(encode_workspace_bytes(c, pts), plain_rescale_limbs(level, n) * c->N * sizeof(u64)));
+}
+// out[g] = rescale(in[g] M_g); ws: plain_steps_bytes of min(groups, KS_MULTI) ciphertexts and as many plaintexts
+static void mask_groups(const ckks_ctx *c, const AttnPlan &p, const ckks_attn_mask &m, const u64 *const *in, u64 *const *out, uint32_t level, void *ws, cudaStream_t s) {
+    const size_t ptw = (size_t)level * c->N;
+    u64 *pts = (u64 *)ws;
+    void *rest = (char *)ws + align256(std::min(p.G, KS_MULTI) * ptw * sizeof(u64));
+    for (uint32_t g0 = 0; g0 < p.G; g0 += KS_MULTI) {
+        const uint32_t nb = std::min(KS_MULTI, p.G - g0);
+        const SlotScores slots{p.Tk, p.H, p.E, p.Ti, p.R, g0, m.causal, m.key_begin, m.key_end, m.window, (long long)m.query_offset};
+        PlainRescale a{};
+        a.in.n = a.out.n = nb;
+        for (uint32_t b = 0; b < nb; b++) { a.in.p[b] = in[g0 + b]; a.out.p[b] = out[g0 + b]; }
+        a.pt = Ptrs(pts, ptw);
+        a.pitch = a.level = level;
+        launch_encode_slots(c, slots, nb, (double)c->mod[level - 1], rest, s);
+        launch_encode_coefs(c, rest, nb, 0, nb, level, false, pts, s);
+        launch_plain_rescale(c, a, (u64 *)rest, s, nb);
+    }
+}
+// out[g] = x[g] without its last limb - rescale(y[g] W)
+static void difference_groups(const ckks_ctx *c, const AttnPlan &p, const double *weights, const ckks_ct *x, const ckks_ct *y, ckks_ct *out, uint32_t level, void *ws,
+                              cudaStream_t s) {
+    u64 *pt = (u64 *)ws;
+    void *rest = (char *)ws + align256((size_t)level * c->N * sizeof(u64));
+    launch_encode_slots(c, SlotHeads{weights, p.H, p.Ti, p.R}, 1, (double)c->mod[level - 1], rest, s);
+    launch_encode_coefs(c, rest, 1, 0, 1, level, false, pt, s);
+    for (uint32_t g0 = 0; g0 < p.G; g0 += KS_MULTI) {
+        const uint32_t nb = std::min(KS_MULTI, p.G - g0);
+        PlainRescale a{};
+        a.in.n = a.acc.n = a.out.n = nb;
+        for (uint32_t b = 0; b < nb; b++) {
+            a.in.p[b] = (const u64 *)y[g0 + b].data; a.acc.p[b] = (const u64 *)x[g0 + b].data; a.out.p[b] = (const u64 *)out[g0 + b].data;
+        }
+        a.pt = Ptrs(pt, 0);
+        a.pitch = a.acc_pitch = a.level = level; a.add = true;
+        launch_plain_rescale(c, a, (u64 *)rest, s, nb);
+    }
+}
+// results may not lie on inputs or on each other
+static bool results_apart(const ckks_ctx *c, uint32_t level, const ckks_ct *const *in, uint32_t nin, const ckks_ct *out, uint32_t G) {
+    const size_t bi = (size_t)2 * level * c->N * sizeof(u64), bo = (size_t)2 * (level - 1) * c->N * sizeof(u64);
+    for (uint32_t g = 0; g < G; g++)
+        for (uint32_t h = 0; h < G; h++) {
+            for (uint32_t x = 0; x < nin; x++)
+                if (!apart(out[g].data, bo, in[x][h].data, bi)) return false;
+            if (g != h && !apart(out[g].data, bo, out[h].data, bo)) return false;
+        }
+    return true;
+}
+
+extern "C" size_t ckks_attention_mask_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
+    AttnPlan p;
+    if (!c || level < 2 || level > c->L || make_attn_plan(c, d, p)) return 0;
+    return plain_steps_bytes(c, level, std::min(p.G, KS_MULTI), std::min(p.G, KS_MULTI));
+}
+
+extern "C" int32_t ckks_attention_mask(ckks_ctx *c, const ckks_attn_desc *d, const ckks_attn_mask *m, const ckks_ct *in, ckks_ct *out, void *ws, size_t ws_bytes,
+                                       void *stream) {
+    if (!c || !out) return CKKS_ERR_ARG;
+    AttnPlan p;
+    int rc = make_attn_plan(c, d, p);
+    if (rc) return rc;
+    if (!mask_ok(p, m)) return CKKS_ERR_ARG;
+    uint32_t level;
+    if ((rc = check_cts(c, in, p.G, &level, false))) return rc;
+    if (level < 2) return CKKS_ERR_LEVEL;
+    for (uint32_t g = 0; g < p.G; g++)
+        if (!out[g].data) return CKKS_ERR_ARG;
+    if (!results_apart(c, level, &in, 1, out, p.G)) return CKKS_ERR_ARG;
+    if (!ws || ws_bytes < ckks_attention_mask_workspace_bytes(c, d, level)) return CKKS_ERR_WORKSPACE;
+    std::vector<const u64 *> vi;
+    std::vector<u64 *> vo;
+    for (uint32_t g = 0; g < p.G; g++) { vi.push_back((const u64 *)in[g].data); vo.push_back((u64 *)out[g].data); }
+    DeviceGuard guard(c->device);
+    mask_groups(c, p, *m, vi.data(), vo.data(), level, ws, (cudaStream_t)stream);
+    rc = finish(c);
+    for (uint32_t g = 0; g < p.G && rc == CKKS_OK; g++) { out[g].level = level - 1; out[g].ncomp = 2; out[g].scale = in[g].scale; }
+    return rc;
+}
+
+extern "C" size_t ckks_attention_difference_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
+    AttnPlan p;
+    if (!c || level < 2 || level > c->L || make_attn_plan(c, d, p)) return 0;
+    return plain_steps_bytes(c, level, std::min(p.G, KS_MULTI), 1);
+}
+
+extern "C" int32_t ckks_attention_difference(ckks_ctx *c, const ckks_attn_desc *d, const ckks_ct *x, const ckks_ct *y, const double *weights, ckks_ct *out, void *ws,
+                                             size_t ws_bytes, void *stream) {
+    if (!c || !out || !weights) return CKKS_ERR_ARG;
+    AttnPlan p;
+    int rc = make_attn_plan(c, d, p);
+    if (rc) return rc;
+    uint32_t level, ly;
+    if ((rc = check_cts(c, x, p.G, &level, true)) || (rc = check_cts(c, y, p.G, &ly, true))) return rc;
+    if (ly != level || level < 2) return CKKS_ERR_LEVEL;
+    for (uint32_t g = 0; g < p.G; g++) {
+        if (!out[g].data) return CKKS_ERR_ARG;
+        if (!scales_agree(x[g].scale, y[g].scale)) return CKKS_ERR_SCALE;
+    }
+    const ckks_ct *ins[2] = {x, y};
+    if (!results_apart(c, level, ins, 2, out, p.G)) return CKKS_ERR_ARG;
+    if (!ws || ws_bytes < ckks_attention_difference_workspace_bytes(c, d, level)) return CKKS_ERR_WORKSPACE;
+    DeviceGuard guard(c->device);
+    difference_groups(c, p, weights, x, y, out, level, ws, (cudaStream_t)stream);
+    rc = finish(c);
+    for (uint32_t g = 0; g < p.G && rc == CKKS_OK; g++) { out[g].level = level - 1; out[g].ncomp = 2; out[g].scale = x[g].scale; }
+    return rc;
+}
+
 // ---- Softmax over rows spread across the groups ---------------------------------------------------------------------
 static bool rows_desc_ok(const ckks_softmax_desc *s) {
     return s && s->exp_coeffs && s->exp_degree >= 2 && (s->rounds == 0 || (s->rsqrt_coeffs && s->rsqrt_degree >= 2));
@@ -225,74 +348,82 @@ extern "C" size_t ckks_softmax_rows_workspace_bytes(const ckks_ctx *c, const ckk
     return (size_t)(2 * p.G + 3) * ct_bytes(c, level) + rows_scratch(c, p, s, level);
 }
 
-extern "C" int32_t ckks_softmax_rows(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_ct *in, const ckks_evk *rlk,
-                                     const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
-    if (!c || !out || !rows_desc_ok(s)) return CKKS_ERR_ARG;
-    AttnPlan p;
-    int rc = make_attn_plan(c, d, p);
-    if (rc) return rc;
-    uint32_t level;
-    if ((rc = check_cts(c, in, p.G, &level, true))) return rc;
-    const uint32_t de = log2_ceil(s->exp_degree), dr = s->rounds ? log2_ceil(s->rsqrt_degree) : 0;
-    if (level < (de + 1) + s->rounds * (dr + 4) + 1) return CKKS_ERR_LEVEL;
-    if (!rlk_ok(rlk)) return CKKS_ERR_NO_KEY;
-    for (int64_t r : p.lad)
-        if (s->rounds && (!keys || !find_key(c, keys, nkeys, r))) return CKKS_ERR_NO_KEY;
-    for (uint32_t g = 0; g < p.G; g++)
-        if (!out[g].data) return CKKS_ERR_ARG;
-    if (!ws || ws_bytes < ckks_softmax_rows_workspace_bytes(c, d, s, level)) return CKKS_ERR_WORKSPACE;
-    // every plan (levels, scales, constants) before anything is launched.  The groups' scales agree within 2^-30 and need not be
-    // equal: every u_g has a scale of its own, and the exponential's constants depend on it.
+// Levels that the Softmax takes from its input, and its levels, scales and constants.  The groups' scales agree within 2^-30 and need not be
+// equal: every u_g has a scale of its own, and the exponential's constants depend on it.
+static uint32_t rows_levels(const ckks_softmax_desc *s, bool masked) {
+    return log2_ceil(s->exp_degree) + 1 + s->rounds * ((s->rounds ? log2_ceil(s->rsqrt_degree) : 0) + 4) + (masked ? 1 : 0);
+}
+struct RowsPlan {
     struct Run { uint32_t g0, n; long long shift; TreePlan poly; };       // neighbours of one scale
-    std::vector<Run> runs;
-    std::vector<double> su(p.G);
-    for (uint32_t g0 = 0; g0 < p.G;) {
-        Run r{g0, 1, 0, TreePlan()};
-        while (r.n < KS_MULTI && g0 + r.n < p.G && in[g0 + r.n].scale == in[g0].scale) r.n++;
-        if (!const_value(-s->shift, in[g0].scale, &r.shift)) return CKKS_ERR_RANGE;
-        if ((rc = poly_tree_plan(c, level, in[g0].scale, s->exp_coeffs, s->exp_degree, r.poly))) return rc;
-        for (uint32_t g = 0; g < r.n; g++) su[g0 + g] = r.poly.out_scale;
-        g0 += r.n;
-        runs.push_back(std::move(r));
-    }
     struct Round { TreePlan poly; uint32_t lu, lt, lx; };                 // levels of u, of its row sums and of lambda u
-    std::vector<Round> rounds(s->rounds);
-    uint32_t lu = runs[0].poly.Lt - 1;
-    for (uint32_t j = 0; j < s->rounds; j++) {
-        Round &r = rounds[j];
-        r.lu = lu; r.lt = lu - 1;
-        for (uint32_t g = 0; g < p.G; g++)
-            if (!scales_agree(su[g], su[0])) return CKKS_ERR_SCALE;
-        const double st = su[0] * su[0] / (double)c->mod[lu - 1];
-        if ((rc = poly_tree_plan(c, r.lt, st, s->rsqrt_coeffs + (size_t)j * (s->rsqrt_degree + 1), s->rsqrt_degree, r.poly))) return rc;
-        r.lx = r.poly.Lt - 2;
-        for (uint32_t g = 0; g < p.G; g++) {
-            const double sx = r.poly.out_scale * su[g] / (double)c->mod[r.poly.Lt - 2];
-            su[g] = sx * sx / (double)c->mod[r.lx - 1];
-        }
-        lu = r.lx - 1;
+    std::vector<Run> runs;
+    std::vector<Round> rounds;
+    std::vector<double> su;
+    uint32_t level, exp_level, out_level;                                 // of the scores, the exponentials before their mask, the result
+};
+static int rows_plan(const ckks_ctx *c, const AttnPlan &p, const ckks_softmax_desc *s, const std::vector<double> &scales, uint32_t level, bool masked, RowsPlan &r) {
+    if (level < rows_levels(s, masked) + 1) return CKKS_ERR_LEVEL;
+    int rc;
+    r.level = level;
+    r.su.resize(p.G);
+    for (uint32_t g0 = 0; g0 < p.G;) {
+        RowsPlan::Run run{g0, 1, 0, TreePlan()};
+        while (run.n < KS_MULTI && g0 + run.n < p.G && scales[g0 + run.n] == scales[g0]) run.n++;
+        if (!const_value(-s->shift, scales[g0], &run.shift)) return CKKS_ERR_RANGE;
+        if ((rc = poly_tree_plan(c, level, scales[g0], s->exp_coeffs, s->exp_degree, run.poly))) return rc;
+        for (uint32_t g = 0; g < run.n; g++) r.su[g0 + g] = run.poly.out_scale;
+        g0 += run.n;
+        r.runs.push_back(std::move(run));
     }
-    const size_t ctw = ct_bytes(c, level) / sizeof(u64), N = c->N;
+    r.exp_level = r.runs[0].poly.Lt - 1;
+    uint32_t lu = r.exp_level - (masked ? 1 : 0);
+    r.rounds.resize(s->rounds);
+    for (uint32_t j = 0; j < s->rounds; j++) {
+        RowsPlan::Round &rd = r.rounds[j];
+        rd.lu = lu; rd.lt = lu - 1;
+        for (uint32_t g = 0; g < p.G; g++)
+            if (!scales_agree(r.su[g], r.su[0])) return CKKS_ERR_SCALE;
+        const double st = r.su[0] * r.su[0] / (double)c->mod[lu - 1];
+        if ((rc = poly_tree_plan(c, rd.lt, st, s->rsqrt_coeffs + (size_t)j * (s->rsqrt_degree + 1), s->rsqrt_degree, rd.poly))) return rc;
+        rd.lx = rd.poly.Lt - 2;
+        for (uint32_t g = 0; g < p.G; g++) {
+            const double sx = rd.poly.out_scale * r.su[g] / (double)c->mod[rd.poly.Lt - 2];
+            r.su[g] = sx * sx / (double)c->mod[rd.lx - 1];
+        }
+        lu = rd.lx - 1;
+    }
+    r.out_level = lu;
+    return CKKS_OK;
+}
+// ws: ckks_softmax_rows_workspace_bytes at the plan's level
+static void rows_run(const ckks_ctx *c, const AttnPlan &p, const RowsPlan &plan, const ckks_attn_mask *mask, const ckks_ct *in, const u64 *rd, const ckks_evk *keys,
+                     uint32_t nkeys, ckks_ct *out, void *ws, cudaStream_t st) {
+    const size_t ctw = ct_bytes(c, plan.level) / sizeof(u64), N = c->N;
+    const uint32_t rounds = (uint32_t)plan.rounds.size();
     u64 *U = (u64 *)ws, *X = U + p.G * ctw, *T = X + p.G * ctw, *T2 = T + ctw, *B = T2 + ctw;
     void *sw = B + ctw;
-    const u64 *rd = (const u64 *)rlk->data;
-    cudaStream_t st = (cudaStream_t)stream;
-    DeviceGuard guard(c->device);
     // u = p_exp(x - shift); all inputs are read before the first result, which may lie on any of them
-    for (const Run &r : runs) {
+    for (const RowsPlan::Run &r : plan.runs) {
         Ptrs pi;
         pi.n = r.n;
         for (uint32_t g = 0; g < r.n; g++) pi.p[g] = (const u64 *)in[r.g0 + g].data;
-        launch_const(c, pi, r.shift, false, Ptrs(X + r.g0 * ctw, ctw), 2, level, st, r.n);
+        launch_const(c, pi, r.shift, false, Ptrs(X + r.g0 * ctw, ctw), 2, plan.level, st, r.n);
     }
-    for (const Run &r : runs) {
+    for (const RowsPlan::Run &r : plan.runs) {
         Ptrs po;
         po.n = r.n;
-        for (uint32_t g = 0; g < r.n; g++) po.p[g] = s->rounds ? U + (size_t)(r.g0 + g) * ctw : (const u64 *)out[r.g0 + g].data;
+        for (uint32_t g = 0; g < r.n; g++) po.p[g] = rounds || mask ? U + (size_t)(r.g0 + g) * ctw : (const u64 *)out[r.g0 + g].data;
         poly_tree_run(c, r.poly, Ptrs(X + r.g0 * ctw, ctw), po, r.n, rd, sw, st);
     }
-    for (uint32_t j = 0; j < s->rounds; j++) {
-        const Round &r = rounds[j];
+    if (mask) {     // what a query does not see leaves its row here: neither the sums nor the values meet it
+        std::vector<const u64 *> vi;
+        std::vector<u64 *> vo;
+        for (uint32_t g = 0; g < p.G; g++) { vi.push_back(U + g * ctw); vo.push_back(rounds ? X + g * ctw : (u64 *)out[g].data); }
+        mask_groups(c, p, *mask, vi.data(), vo.data(), plan.exp_level, sw, st);
+        std::swap(U, X);
+    }
+    for (uint32_t j = 0; j < rounds; j++) {
+        const RowsPlan::Round &r = plan.rounds[j];
         // t = row sums of u^2: one relinearisation for the sum over the groups, then the ladder over the blocks, back and forth
         std::vector<CtView> u;
         for (uint32_t g = 0; g < p.G; g++) u.push_back(CtView{U + g * ctw, (size_t)r.lu * N});
@@ -311,14 +442,50 @@ extern "C" int32_t ckks_softmax_rows(ckks_ctx *c, const ckks_attn_desc *d, const
         for (uint32_t g = 0; g < p.G; g++) {
             xo.push_back(X + g * ctw);
             x.push_back(CtView{X + g * ctw, (size_t)r.lx * N});
-            uo.push_back(j + 1 == s->rounds ? (u64 *)out[g].data : U + g * ctw);
+            uo.push_back(j + 1 == rounds ? (u64 *)out[g].data : U + g * ctw);
         }
         mul_rescale(c, lam.data(), u.data(), xo.data(), p.G, rd, lb, sw, KS_MULTI, st);
         mul_rescale(c, x.data(), x.data(), uo.data(), p.G, rd, r.lx, sw, KS_MULTI, st);
     }
+    for (uint32_t g = 0; g < p.G; g++) { out[g].level = plan.out_level; out[g].ncomp = 2; out[g].scale = plan.su[g]; }
+}
+
+static int softmax_rows(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_attn_mask *mask, const ckks_ct *in, const ckks_evk *rlk,
+                        const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
+    if (!c || !out || !rows_desc_ok(s)) return CKKS_ERR_ARG;
+    AttnPlan p;
+    int rc = make_attn_plan(c, d, p);
+    if (rc) return rc;
+    if (mask && !mask_ok(p, mask)) return CKKS_ERR_ARG;
+    uint32_t level;
+    if ((rc = check_cts(c, in, p.G, &level, true))) return rc;
+    if (level < rows_levels(s, mask != nullptr) + 1) return CKKS_ERR_LEVEL;
+    if (!rlk_ok(rlk)) return CKKS_ERR_NO_KEY;
+    for (int64_t r : p.lad)
+        if (s->rounds && (!keys || !find_key(c, keys, nkeys, r))) return CKKS_ERR_NO_KEY;
+    for (uint32_t g = 0; g < p.G; g++)
+        if (!out[g].data) return CKKS_ERR_ARG;
+    if (!ws || ws_bytes < ckks_softmax_rows_workspace_bytes(c, d, s, level)) return CKKS_ERR_WORKSPACE;
+    RowsPlan plan;
+    std::vector<double> scales;
+    for (uint32_t g = 0; g < p.G; g++) scales.push_back(in[g].scale);
+    if ((rc = rows_plan(c, p, s, scales, level, mask != nullptr, plan))) return rc;
+    DeviceGuard guard(c->device);
+    std::vector<ckks_ct> o(out, out + p.G);          // the descriptors change once nothing has failed
+    rows_run(c, p, plan, mask, in, (const u64 *)rlk->data, keys, nkeys, o.data(), ws, (cudaStream_t)stream);
     rc = finish(c);
-    for (uint32_t g = 0; g < p.G && rc == CKKS_OK; g++) { out[g].level = lu; out[g].ncomp = 2; out[g].scale = su[g]; }
+    for (uint32_t g = 0; g < p.G && rc == CKKS_OK; g++) out[g] = o[g];
     return rc;
+}
+
+extern "C" int32_t ckks_softmax_rows(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_ct *in, const ckks_evk *rlk,
+                                     const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
+    return softmax_rows(c, d, s, nullptr, in, rlk, keys, nkeys, out, ws, ws_bytes, stream);
+}
+extern "C" int32_t ckks_softmax_rows_masked(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_attn_mask *mask, const ckks_ct *in,
+                                            const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
+    if (!mask) return CKKS_ERR_ARG;
+    return softmax_rows(c, d, s, mask, in, rlk, keys, nkeys, out, ws, ws_bytes, stream);
 }
 
 // ---- probability x value ------------------------------------------------------------------------------------------
@@ -429,6 +596,94 @@ extern "C" int32_t ckks_attention(ckks_ctx *c, const ckks_attn_desc *d, const ck
     if ((rc = ckks_attention_scores(c, d, q, k, dim, rlk, keys, nkeys, S.data(), sw, sw_bytes, stream))) return rc;
     if ((rc = ckks_softmax_rows(c, d, s, S.data(), rlk, keys, nkeys, P.data(), sw, sw_bytes, stream))) return rc;
     return ckks_attention_values(c, d, P.data(), v, dim_v, rlk, keys, nkeys, out, sw, sw_bytes, stream);
+}
+
+// ---- masked attention, and the difference of two maps ------------------------------------------------------------------
+// Workspace: the score maps and their probabilities (the difference lies where the first scores were), the scratch of the steps.
+// Everything is checked and planned before the first launch.
+static size_t maps_bytes(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, uint32_t level, uint32_t dim, uint32_t maps) {
+    AttnPlan p;
+    if (!c || level < 3 || level > c->L || !dim || !rows_desc_ok(s) || make_attn_plan(c, d, p)) return 0;
+    return (size_t)(1 + maps) * p.G * ct_bytes(c, level - 1) +
+           std::max({ckks_attention_scores_workspace_bytes(c, d, level, dim), ckks_softmax_rows_workspace_bytes(c, d, s, level - 1),
+                     plain_steps_bytes(c, level - 1, std::min(p.G, KS_MULTI), 1), ckks_attention_values_workspace_bytes(c, d, level - 1)});
+}
+static int attend(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_attn_mask *mask, const double *weights, uint32_t maps,
+                  const ckks_ct *const *q, const ckks_ct *const *k, uint32_t dim, const ckks_ct *v, uint32_t dim_v, const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys,
+                  ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
+    if (!c || !out || !rows_desc_ok(s)) return CKKS_ERR_ARG;
+    AttnPlan p;
+    int rc = make_attn_plan(c, d, p);
+    if (rc) return rc;
+    if (mask && !mask_ok(p, mask)) return CKKS_ERR_ARG;
+    uint32_t level = 0, lv;
+    for (uint32_t m = 0; m < maps; m++)
+        for (const ckks_ct *x : {q[m], k[m]}) {
+            uint32_t l;
+            if ((rc = check_cts(c, x, dim, &l, true))) return rc;
+            if (level && l != level) return CKKS_ERR_LEVEL;
+            level = l;
+        }
+    if ((rc = check_cts(c, v, dim_v, &lv, true))) return rc;
+    if (maps == 2 && !scales_agree(q[0][0].scale * k[0][0].scale, q[1][0].scale * k[1][0].scale)) return CKKS_ERR_SCALE;
+    // scores, Softmax, difference, values
+    const uint32_t lost = 1 + rows_levels(s, mask != nullptr) + (maps - 1);
+    if (level < lost + 2 || lv < level - lost) return CKKS_ERR_LEVEL;
+    if (!rlk_ok(rlk)) return CKKS_ERR_NO_KEY;
+    for (const std::vector<int64_t> *list : {&p.tok, &p.lad, &p.neg})
+        for (int64_t r : *list)
+            if (!keys || !find_key(c, keys, nkeys, r)) return CKKS_ERR_NO_KEY;
+    for (uint32_t x = 0; x < dim_v; x++)
+        if (!out[x].data) return CKKS_ERR_ARG;
+    const size_t need = maps_bytes(c, d, s, level, dim, maps), ctb = ct_bytes(c, level - 1);
+    if (!ws || !need || ws_bytes < need) return CKKS_ERR_WORKSPACE;
+    RowsPlan plan[2];
+    for (uint32_t m = 0; m < maps; m++) {
+        const std::vector<double> scales(p.G, q[m][0].scale * k[m][0].scale / (double)c->mod[level - 1]);
+        if ((rc = rows_plan(c, p, s, scales, level - 1, mask != nullptr, plan[m]))) return rc;
+    }
+    char *base = (char *)ws;
+    auto map = [&](uint32_t m) {
+        std::vector<ckks_ct> x(p.G);
+        for (uint32_t g = 0; g < p.G; g++) x[g] = ckks_ct{(uint64_t *)(base + ((size_t)m * p.G + g) * ctb), level - 1, 2, 0.0};
+        return x;
+    };
+    std::vector<ckks_ct> S = map(0), P[2] = {map(1), map(maps)};
+    void *sw = base + (size_t)(1 + maps) * p.G * ctb;
+    const size_t sw_bytes = ws_bytes - (size_t)(1 + maps) * p.G * ctb;
+    DeviceGuard guard(c->device);
+    for (uint32_t m = 0; m < maps; m++) {
+        for (ckks_ct &x : S) x.level = level - 1;
+        if ((rc = ckks_attention_scores(c, d, q[m], k[m], dim, rlk, keys, nkeys, S.data(), sw, sw_bytes, stream))) return rc;
+        rows_run(c, p, plan[m], mask, S.data(), (const u64 *)rlk->data, keys, nkeys, P[m].data(), sw, (cudaStream_t)stream);
+    }
+    const ckks_ct *probs = P[0].data();
+    if (maps == 2) {
+        difference_groups(c, p, weights, P[0].data(), P[1].data(), S.data(), plan[0].out_level, sw, (cudaStream_t)stream);
+        for (uint32_t g = 0; g < p.G; g++) { S[g].level = plan[0].out_level - 1; S[g].ncomp = 2; S[g].scale = P[0][g].scale; }
+        probs = S.data();
+    }
+    return ckks_attention_values(c, d, probs, v, dim_v, rlk, keys, nkeys, out, sw, sw_bytes, stream);
+}
+
+extern "C" size_t ckks_attention_masked_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, uint32_t level, uint32_t dim) {
+    return maps_bytes(c, d, s, level, dim, 1);
+}
+extern "C" int32_t ckks_attention_masked(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_attn_mask *mask, const ckks_ct *q, const ckks_ct *k,
+                                         uint32_t dim, const ckks_ct *v, uint32_t dim_v, const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws,
+                                         size_t ws_bytes, void *stream) {
+    if (!mask) return CKKS_ERR_ARG;
+    return attend(c, d, s, mask, nullptr, 1, &q, &k, dim, v, dim_v, rlk, keys, nkeys, out, ws, ws_bytes, stream);
+}
+extern "C" size_t ckks_attention_differential_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, uint32_t level, uint32_t dim) {
+    return maps_bytes(c, d, s, level, dim, 2);
+}
+extern "C" int32_t ckks_attention_differential(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_attn_mask *mask, const double *weights,
+                                               const ckks_ct *q1, const ckks_ct *k1, const ckks_ct *q2, const ckks_ct *k2, uint32_t dim, const ckks_ct *v, uint32_t dim_v,
+                                               const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
+    if (!weights) return CKKS_ERR_ARG;
+    const ckks_ct *q[2] = {q1, q2}, *k[2] = {k1, k2};
+    return attend(c, d, s, mask, weights, 2, q, k, dim, v, dim_v, rlk, keys, nkeys, out, ws, ws_bytes, stream);
 }
 
 // ---- conversion between the projections' token-shard layout and the attention operands ---------------------------------

@@ -367,6 +367,7 @@ inline bool aligned16(const Ptrs &p) {
 //           map's periods are the entries' components)
 //   mode 2: the transform's own result is stored, but into a tiled buffer (out.base): limb y = b * level + i becomes row
 //           tl.row0 + b * tl.row_stride, limb i
+//   mode 4: as mode 1 with u[b][comp][i][p] times the plaintext pt.at(b)[i][p] in u's place
 constexpr uint32_t IP_FUSED_BETA = 4;
 struct NttEpilogue {
     int mode;
@@ -375,6 +376,8 @@ struct NttEpilogue {
     uint32_t add_comps, ncomp, level, nt;
     u64 galois;
     int accumulate;        // acc is given
+    uint32_t acc_pitch;    // limbs between the components of acc (0: level)
+    Ptrs pt;               // mode 4
     TiledOut tl;
     int multi;             // batch entry b adds through mgalois[b]
     u64 mgalois[KS_MULTI];
@@ -399,9 +402,12 @@ struct NttPrologue {
 };
 // Source of the inverse transform: the first pass reads limb x of entry b at ptr.at(b) + x * lpitch limbs, so the transform
 // runs out of place and the input stays as it is (b = limb index / map.period, x = limb index % map.period).
+// mul (may be null): every word is multiplied by the same word of limb mul.at(b) on the way (rows by a warp only).
 struct NttSource {
     Ptrs ptr;
     uint32_t lpitch = 0;
+    Ptrs mul;
+    uint32_t has_mul = 0;
 };
 // alone: the chain of launches belongs to a short call of its own, which for a small ring the host bounds: fewest launches.
 // inv_scale (inverse): pairs [map.period][2] that replace {N^-1, last twiddle N^-1} for limb x of every period (device
@@ -492,6 +498,9 @@ void ks_apply(const ckks_ctx *c, const u64 *evk, uint32_t level, const KsWorkspa
 // out = rescale(ModDown(<digits, key>) + add), level - 1 limbs per component, without the tensor-core conversions (see ks_fused_rescale)
 void ks_apply_rescale(const ckks_ctx *c, const u64 *evk, uint32_t level, const KsWorkspace &w, const Ptrs &add, const Ptrs &out, cudaStream_t s, uint32_t nb);
 bool ks_fused_rescale(const ckks_ctx *c);
+// out = rescale(ModDown(w.u)) (+ acc: [2][level - 1][N] words per entry, possibly out itself); w.mid: the limbs of u from level - 1 on are
+// left after the inverse row pass
+void ks_down_rescale(const ckks_ctx *c, uint32_t level, const KsWorkspace &w, const Ptrs &out, const Ptrs *acc, cudaStream_t s, uint32_t nb);
 // A sum of up to IP_TERMS key-switched terms in one pass over the extended basis:
 //   u[b] (+)= sum_t ( <ext[t][b] read through sigma_{g_t}, evk_t>  +  P sigma_{g_t}(c0_t[b]) on component 0's q-limbs )
 // ext holds term t's digits of batch entry b at ext + t * term_stride + b * beta * (level + K) * N words, the own limbs of the
@@ -521,6 +530,21 @@ struct MidArgs {
     int has_add, acc_u;
 };
 void launch_mid_rows(const ckks_ctx *c, const MidArgs &a, uint32_t beta, cudaStream_t s);
+// Key switches of rotations whose results are multiplied by plaintexts, in the extended basis (positions.cu), with what is added to them:
+//   u[b][k] = sum_{r < nrot} S_r ( <ext[b] read through sigma_r, evk_r>_k + [k = 0] P sigma_r(c0) ) + P C c_k,   c = c[b],
+// S_r of set s at fac + r fac_rot + s fac_set ([level + K][N]), C at own + s own_set ([level][N]), s = set[b]; the terms with P on the
+// q-limbs alone.  Component 1 of c[b] lies `pitch` limbs behind component 0; digits that have a limb among their own read it there.
+constexpr uint32_t POS_ROT = 2;
+struct PosArgs {
+    const u64 *ext, *evk[POS_ROT], *own, *fac;
+    u64 galois[POS_ROT];
+    Ptrs c;
+    u64 *u;
+    size_t own_set, fac_set, fac_rot;
+    uint32_t pitch, nrot, nb, level, inv_from;
+    uint8_t set[KS_MULTI];
+};
+void launch_mid_rows_pos(const ckks_ctx *c, const PosArgs &a, uint32_t beta, cudaStream_t s);
 // The basis conversions on the tensor cores (contexts with byte matrices: at most 8 sources)
 void launch_modup_mma(const ckks_ctx *c, const u64 *dcoef, u64 *ext, uint32_t level, uint32_t nb, cudaStream_t s);
 void launch_moddown_conv_mma(const ckks_ctx *c, const u64 *u, u64 *conv, uint32_t level, uint32_t nb, cudaStream_t s);
@@ -554,11 +578,47 @@ bool launch_mac_umma(const ckks_ctx *c, const u64 *baby, const u64 *pts, u64 *ac
 void launch_rescale(const ckks_ctx *c, const Ptrs &in, const Ptrs &out, uint32_t ncomp, uint32_t level, u64 *ws, cudaStream_t s, uint32_t nb = 1,
                     bool alone = false);
 
+// out[b] = rescale(in[b] pt[b]) (+ acc[b], a ciphertext of level - 1 limbs whose components lie acc_pitch limbs apart) for nb <= KS_MULTI
+// two-component ciphertexts, the components of in[b] `pitch` limbs apart; ws: plain_rescale_limbs
+struct PlainRescale {
+    Ptrs in, pt, acc, out;
+    uint32_t pitch, acc_pitch, level;
+    bool add;
+};
+inline size_t plain_rescale_limbs(uint32_t level, uint32_t nb) { return (size_t)nb * 2 * level; }
+void launch_plain_rescale(const ckks_ctx *c, const PlainRescale &a, u64 *ws, cudaStream_t s, uint32_t nb);
+
 size_t encode_workspace_bytes(const ckks_ctx *c, uint32_t batch);
 // tiled.R != 0: plaintext b is written as row tiled.row0 + b * tiled.row_stride of the tiled buffer
 // `tiled_out`; `out` is then only the scratch between the two NTT passes.
 void launch_encode(const ckks_ctx *c, const double *re, const double *im, uint32_t batch, double scale, uint32_t level,
                    u64 *out, void *ws, cudaStream_t s, TiledOut tiled = TiledOut(), u64 *tiled_out = nullptr);
+// Slot values formed where the encoder reads them, plaintext b of a batch of at most SLOT_SETS sets (times 1 + POS_ROT for positions).
+constexpr uint32_t SLOT_SETS = KS_MULTI;
+// Position factors of shard ciphertexts, slot ((copy dim + d) heads + h) inner + t.  b = kind * sets + set, kind 0: the factor of a channel
+// itself, 1, ..: of its partner under rotation kind - 1.  Token t of begin <= t < end takes row + (t - begin) step of the tables
+// [..][rot / 2], the others zeros.
+struct SlotPositions {
+    const double *cos, *sin;
+    uint32_t dim, heads, inner, rot, interleaved, step, sets, nrot;
+    uint32_t row[SLOT_SETS], begin[SLOT_SETS], end[SLOT_SETS];
+};
+// 1.0 for the tokens begin <= t < end of a shard ciphertext
+struct SlotTokens { uint32_t inner, begin[SLOT_SETS], end[SLOT_SETS]; };
+// Score ciphertexts, slot ((((e P + pos) heads + h) inner + t) copies + r): 1.0 where query i sees the key token of group g0 + b
+struct SlotScores {
+    uint32_t tokens, heads, block, inner, copies, g0;
+    uint32_t causal, key_begin, key_end, window;
+    long long offset;
+};
+// -weights[h] (device)
+struct SlotHeads { const double *weights; uint32_t heads, inner, copies; };
+// out: [batch][level][N], or with `special` [batch][level + K][N]; batch <= 65535 plaintexts whose coefficients are formed by
+// launch_encode_slots in ws (encode_workspace_bytes) and transformed by launch_encode_coefs, `first` plaintexts into them
+template <class Slots>
+void launch_encode_slots(const ckks_ctx *c, const Slots &slots, uint32_t batch, double scale, void *ws, cudaStream_t s);
+void launch_encode_coefs(const ckks_ctx *c, const void *ws, uint32_t batch, uint32_t first, uint32_t count, uint32_t level, bool special, u64 *out,
+                         cudaStream_t s);
 // Slot vectors of generalised diagonals, [count][n] fp64, for k = k0 .. k0+count-1 of one block pair, diagonal k pre-rotated by its
 // giant step's share k - k % B.
 void launch_extract_diagonals(const ckks_ctx *c, const double *W, uint32_t d_out_total, uint32_t in0, uint32_t m_in,

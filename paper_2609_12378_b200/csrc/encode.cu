@@ -26,17 +26,54 @@ __device__ __forceinline__ double2 cmul_conj_w(double2 w, double2 v) {   // conj
     return make_double2(__dsub_rn(p0, p1), __dadd_rn(p2, p3));
 }
 
+// ---- what a slot holds: an array's value, or one formed here (a launch and a trip through memory less) ---------------------
+struct SlotArray { const double *re, *im; };
+__device__ __forceinline__ double2 slot_value(const SlotArray &a, uint32_t b, uint32_t j, uint32_t n) {
+    return make_double2(a.re[(size_t)b * n + j], a.im ? a.im[(size_t)b * n + j] : 0.0);
+}
+__device__ __forceinline__ double2 slot_value(const SlotPositions &a, uint32_t b, uint32_t j, uint32_t) {
+    const uint32_t kind = b / a.sets, set = b % a.sets, t = j % a.inner, d = j / (a.inner * a.heads) % a.dim, half = a.rot / 2;
+    if (t < a.begin[set] || t >= a.end[set]) return make_double2(0.0, 0.0);
+    if (d >= a.rot) return make_double2(kind ? 0.0 : 1.0, 0.0);
+    const uint32_t pair = a.interleaved ? d >> 1 : d % half;
+    const bool second = a.interleaved ? d & 1 : d >= half;
+    const size_t at = ((size_t)a.row[set] + (size_t)(t - a.begin[set]) * a.step) * half + pair;
+    if (!kind) return make_double2(a.cos[at], 0.0);
+    // one rotation serves both channels of a pair; of two, the first (to the left) serves the first channel, the other the second
+    if (a.nrot == 2 && second != (kind == 2)) return make_double2(0.0, 0.0);
+    return make_double2(second ? a.sin[at] : -a.sin[at], 0.0);
+}
+__device__ __forceinline__ double2 slot_value(const SlotTokens &a, uint32_t b, uint32_t j, uint32_t) {
+    const uint32_t t = j % a.inner;
+    return make_double2(t >= a.begin[b] && t < a.end[b] ? 1.0 : 0.0, 0.0);
+}
+__device__ __forceinline__ double2 slot_value(const SlotScores &a, uint32_t b, uint32_t j, uint32_t) {
+    const uint32_t x = j / a.copies, pos = x / (a.inner * a.heads), per = a.tokens / a.inner;
+    const uint32_t e = pos / per, i = pos % per * a.inner + x % a.inner;
+    // the key operand holds token (i + e) mod tokens in block e; group g is its rotation by g blocks' tokens over (e, i)
+    uint32_t f = i + (a.g0 + b) * a.block, fe = e;
+    if (f >= a.tokens) { f -= a.tokens; fe = e + 1 == a.block ? 0 : e + 1; }
+    const uint32_t key = (f + fe) % a.tokens;
+    const long long at = (long long)i + a.offset;
+    const bool live = key >= a.key_begin && key < a.key_end && (!a.causal || (long long)key <= at) && (!a.window || (long long)key > at - (long long)a.window);
+    return make_double2(live ? 1.0 : 0.0, 0.0);
+}
+__device__ __forceinline__ double2 slot_value(const SlotHeads &a, uint32_t, uint32_t j, uint32_t) {
+    return make_double2(-a.weights[j / (a.copies * a.inner) % a.heads], 0.0);
+}
+
 // Pass 1: gather (E1 + bit reversal), stages m = 2 .. min(n, CH) on chunks of CH points.  The stages' twiddles come from
 // a copy in shared memory (stage by stage, so that a warp reads consecutive entries): fetched from the full table they
 // were 5120 scattered 16-byte loads per CTA and the kernel was bound by the traffic between L2 and L1.
-__global__ void __launch_bounds__(THREADS) fft_chunks(DevTables c, const double *re, const double *im, double2 *buf, uint32_t n, uint32_t ch) {
+template <class Src>
+__global__ void __launch_bounds__(THREADS) fft_chunks(DevTables c, const __grid_constant__ Src src, double2 *buf, uint32_t n, uint32_t ch) {
     __shared__ double2 sm[CH];
     __shared__ double2 tw[CH];
     const uint32_t b = blockIdx.y, base = blockIdx.x * ch;
     grid_dep_sync();
     for (uint32_t x = threadIdx.x; x < ch; x += THREADS) {
         const uint32_t j = c.enc_src[base + x];
-        sm[x] = make_double2(re[(size_t)b * n + j], im ? im[(size_t)b * n + j] : 0.0);
+        sm[x] = slot_value(src, b, j, n);
         tw[x] = c.enc_omega_st[x];
     }
     __syncthreads();
@@ -141,7 +178,7 @@ void launch_encode(const ckks_ctx *c, const double *re, const double *im, uint32
     const double sc = scale / (double)n;
     for (uint32_t b0 = 0; b0 < batch; b0 += 32768) {
         const uint32_t nb = batch - b0 < 32768 ? batch - b0 : 32768;
-        launch(fft_chunks, dim3(n / ch, nb), THREADS, 0, s, c->dev, re + (size_t)b0 * n, im ? im + (size_t)b0 * n : nullptr, buf + (size_t)b0 * n, n, ch);
+        launch(fft_chunks<SlotArray>, dim3(n / ch, nb), THREADS, 0, s, c->dev, SlotArray{re + (size_t)b0 * n, im ? im + (size_t)b0 * n : nullptr}, buf + (size_t)b0 * n, n, ch);
         launch(fft_strips_round, dim3(ch / COLS, nb), THREADS, (size_t)2 * (n / ch) * COLS * sizeof(double2), s, c->dev, buf + (size_t)b0 * n, coef + (size_t)b0 * N, n, ch, sc);
     }
     // the first NTT pass reduces the signed coefficients itself; the last one can write the tiled layout
@@ -149,6 +186,27 @@ void launch_encode(const ckks_ctx *c, const double *re, const double *im, uint32
     NttEpilogue ep{};
     ep.mode = 2; ep.out.base = tiled_out; ep.level = level; ep.tl = tiled;
     launch_ntt(c, out, batch * level, plain_map(0, level), false, s, tiled.R ? &ep : nullptr, &pro);
+}
+
+template <class Slots>
+void launch_encode_slots(const ckks_ctx *c, const Slots &slots, uint32_t batch, double scale, void *ws, cudaStream_t s) {
+    const uint32_t n = c->n, ch = n < CH ? n : CH;
+    double2 *buf = (double2 *)ws;
+    long long *coef = (long long *)(buf + (size_t)batch * n);
+    launch(fft_chunks<Slots>, dim3(n / ch, batch), THREADS, 0, s, c->dev, slots, buf, n, ch);
+    launch(fft_strips_round, dim3(ch / COLS, batch), THREADS, (size_t)2 * (n / ch) * COLS * sizeof(double2), s, c->dev, buf, coef, n, ch, scale / (double)n);
+}
+template void launch_encode_slots(const ckks_ctx *, const SlotPositions &, uint32_t, double, void *, cudaStream_t);
+template void launch_encode_slots(const ckks_ctx *, const SlotTokens &, uint32_t, double, void *, cudaStream_t);
+template void launch_encode_slots(const ckks_ctx *, const SlotScores &, uint32_t, double, void *, cudaStream_t);
+template void launch_encode_slots(const ckks_ctx *, const SlotHeads &, uint32_t, double, void *, cudaStream_t);
+
+void launch_encode_coefs(const ckks_ctx *c, const void *ws, uint32_t batch, uint32_t first, uint32_t count, uint32_t level, bool special, u64 *out,
+                         cudaStream_t s) {
+    const long long *coef = (const long long *)((const double2 *)ws + (size_t)batch * c->n) + (size_t)first * c->N;
+    const NttPrologue pro{(const u64 *)coef, false, 0};
+    const uint32_t limbs = level + (special ? c->K : 0);
+    launch_ntt(c, out, count * limbs, special ? tail_map(0, level, c->K, c->L) : plain_map(0, level), false, s, nullptr, &pro);
 }
 
 void launch_extract_diagonals(const ckks_ctx *c, const double *W, uint32_t d_out_total, uint32_t in0, uint32_t m_in,

@@ -675,6 +675,11 @@ bool ks_fused_rescale(const ckks_ctx *c) { return !conv_tensor(c); }
 // ModDown and rescale at once, bit for bit what they give one after the other (see moddown_conv_kernel); the polynomial of
 // degree 63 at N = 2^16, level 24, whose products all end this way: 2615 -> 2295 us.
 void ks_apply_rescale(const ckks_ctx *c, const u64 *evk, uint32_t level, const KsWorkspace &w, const Ptrs &add, const Ptrs &out, cudaStream_t s, uint32_t nb) {
+    if (w.mid) mid_inner(c, evk, level, 1, w, level - 1, s, nb, nullptr, &add);
+    else ks_inner(c, evk, level, 1, w, s, nb, false, nullptr, &add);
+    ks_down_rescale(c, level, w, out, nullptr, s, nb);
+}
+void ks_down_rescale(const ckks_ctx *c, uint32_t level, const KsWorkspace &w, const Ptrs &out, const Ptrs *acc, cudaStream_t s, uint32_t nb) {
     const uint32_t N = c->N, K = c->K, nt = level + K, m = level - 1;
     NttEpilogue ep{};
     ep.mode = 1;
@@ -682,9 +687,8 @@ void ks_apply_rescale(const ckks_ctx *c, const u64 *evk, uint32_t level, const K
     ep.out = out;
     ep.pinv = c->dev.rs_p_inv_d + (size_t)m * c->L;
     ep.ncomp = 2; ep.level = m; ep.nt = nt; ep.galois = 1;
+    if (acc) { ep.acc = *acc; ep.accumulate = 1; }
     const bool strip = conv_strip(c, CONV_DOWN_RS, level, 2 * nb);
-    if (w.mid) mid_inner(c, evk, level, 1, w, m, s, nb, nullptr, &add);
-    else ks_inner(c, evk, level, 1, w, s, nb, false, nullptr, &add);
     // the dropped limb and the K special limbs of every (batch, component), nt limbs apart
     const NttPart first = NttPart((w.mid ? 0 : NTT_ROWS) | (strip ? 0 : NTT_COLS));
     if (first)
@@ -767,4 +771,29 @@ void launch_rescale(const ckks_ctx *c, const Ptrs &in, const Ptrs &out, uint32_t
     ep.pinv = c->dev.rs_inv_d + (size_t)(level - 1) * c->L;
     ep.ncomp = ncomp; ep.level = level - 1; ep.nt = level; ep.galois = 1;
     launch_ntt(c, tmp, nb * ncomp * (level - 1), plain_map(0, level - 1), false, s, &ep, &pro);
+}
+
+// A product with a plaintext and its rescale without the product ever leaving a kernel: the dropped limbs' inverse transform multiplies
+// as it reads, and the last pass of the forward transform as it finishes (mode 4 of the epilogue).
+// ws: [nb][2][N] last limbs + [nb][2][level-1][N]
+void launch_plain_rescale(const ckks_ctx *c, const PlainRescale &a, u64 *ws, cudaStream_t s, uint32_t nb) {
+    const uint32_t m = a.level - 1;
+    const size_t N = c->N;
+    u64 *last = ws, *tmp = ws + (size_t)nb * 2 * N;
+    NttSource src;
+    src.lpitch = a.pitch; src.has_mul = 1;
+    src.ptr.n = src.mul.n = nb;
+    for (uint32_t b = 0; b < nb; b++) {
+        src.ptr.p[b] = a.in.at(b) + m * N;
+        src.mul.p[b] = a.pt.at(b) + m * N;
+    }
+    launch_ntt(c, last, nb * 2, same_map(m, 2), true, s, nullptr, nullptr, &src);
+    NttPrologue pro{last, true, m};
+    NttEpilogue ep{};
+    ep.mode = 4;
+    ep.u = a.in; ep.pt = a.pt; ep.out = a.out;
+    ep.pinv = c->dev.rs_inv_d + (size_t)m * c->L;
+    ep.ncomp = 2; ep.level = m; ep.nt = a.pitch; ep.galois = 1;
+    if (a.add) { ep.acc = a.acc; ep.acc_pitch = a.acc_pitch; ep.accumulate = 1; }
+    launch_ntt(c, tmp, nb * 2 * m, plain_map(0, m), false, s, &ep, &pro);
 }

@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(ColShape<LOGR>::THREADS, 768 / ColShape<LOGR>:
 
 // ---- row passes (see ROW_PAD) --------------------------------------------------------------------------------------------
 // forward, EP 0: in place; 1: the tail of a ModDown or rescale, (u - NTT(conv)) c + sigma_g(add), written to its final
-// place; 2: into a tiled buffer; 3: as 1 with u formed here from BETA digits and the key.  EP 3 is bound by HBM (the key words and the
+// place; 2: into a tiled buffer; 3: as 1 with u formed here from BETA digits and the key; 4: as 1 with u times a plaintext.  EP 3 is bound by HBM (the key words and the
 // results); one pair of words per step at 64 registers: two pairs at 96 registers and 20 warps per SM took 1750 us for 64
 // rotations, four pairs at 128 registers 1910, against 1550.
 template <int EP, bool WIDE, uint32_t BETA = 1>
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(16 * ROW_CTA, 64 / ROW_CTA) ntt_fwd_rows(DevTa
     for (uint32_t k = 0; k < 16; k += 2) *reinterpret_cast<double2 *>(blk + k) = make_double2(x[k], x[k + 1]);
     __syncwarp();
     const double *sp = s + 2 * t + 2 * (t >> 3);          // padded(2 t); word 2 t + 32 k is 36 k further
-    if (EP == 1 || EP == 3) {
+    if (EP == 1 || EP == 3 || EP == 4) {
         const uint32_t y = yl + ep.y0, i = y % ep.level, comp = (y / ep.level) % ep.ncomp, bz = y / (ep.ncomp * ep.level);
         const double2 pinv = ep.pinv[i];
         const uint32_t p0 = row * 256 + 2 * t;
@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(16 * ROW_CTA, 64 / ROW_CTA) ntt_fwd_rows(DevTa
         const uint32_t rot = ep.group ? bz / ep.group : bz, mem = ep.group ? bz % ep.group : bz;
         const uint32_t gal = (uint32_t)(ep.multi ? ep.mgalois[rot] : ep.galois);
         const u64 *add = (ep.add_comps >> comp & 1) ? ep.add.at(ep.own ? bz : mem) + (((size_t)comp * ep.level + i) << c.log_n) : nullptr;
-        const u64 *acc = ep.accumulate ? ep.acc.at(bz) + (((size_t)comp * ep.level + i) << c.log_n) + p0 : nullptr;
+        const u64 *acc = ep.accumulate ? ep.acc.at(bz) + (((size_t)comp * (ep.acc_pitch ? ep.acc_pitch : ep.level) + i) << c.log_n) + p0 : nullptr;
         const uint32_t bstep = ep.tl.R ? ep.tl.R * 64 : 64;    // words from one 64-word block of the destination to the next
         u64 *dst = ep.tl.R ? const_cast<u64 *>(ep.out.base) + tiled_index(ep.tl.R, c.N, ep.tl.row0 + rot * ep.rot_rows + (ep.group ? mem : bz) * ep.tl.row_stride + comp, i, row * 256) + 2 * t
                            : const_cast<u64 *>(ep.group ? ep.out.base + rot * ep.rot_stride + mem * ep.out.stride : ep.out.at(bz)) +
@@ -262,6 +262,7 @@ __global__ void __launch_bounds__(16 * ROW_CTA, 64 / ROW_CTA) ntt_fwd_rows(DevTa
         const u64 *up = ep.u.at(bz) + (((size_t)comp * ep.nt + i) << c.log_n) + p0;
         // the other operands are fetched four pairs at a time, all in flight together (one pair per step, behind the step's
         // arithmetic, was latency bound: 332 us against 243 for 16 key switches at level 24)
+        const u64 *pp = EP == 4 ? ep.pt.at(bz) + ((size_t)i << c.log_n) + p0 : nullptr;
         ulonglong2 ua[4], aa[4];
         uint32_t sr[4];
 #pragma unroll
@@ -270,6 +271,8 @@ __global__ void __launch_bounds__(16 * ROW_CTA, 64 / ROW_CTA) ntt_fwd_rows(DevTa
 #pragma unroll
                 for (uint32_t h = 0; h < 4; h++) {
                     ua[h] = ld_pair<WIDE>(up + 32 * (k + h));
+                    if (EP == 4) aa[h] = ld_pair<WIDE>(pp + 32 * (k + h));
+                    else
                     if (add) {      // the permutation maps the pair onto a pair, possibly swapped
                         sr[h] = galois_src(p0 + 32 * (k + h), gal, c.log_n);
                         aa[h] = ld_pair<WIDE>(add + (sr[h] & ~1u));
@@ -281,9 +284,11 @@ __global__ void __launch_bounds__(16 * ROW_CTA, 64 / ROW_CTA) ntt_fwd_rows(DevTa
             const double2 v = *reinterpret_cast<const double2 *>(sp + 36 * k);
             const ulonglong2 uu = ua[k & 3], a = aa[k & 3];
             // |u - v| < 1.5 q, times P^-1 -> |.| < 0.9 q, plus up to two residues, reduced once
-            double r0 = mulmod_d<0>(__dsub_rn(u64_to_d(uu.x), reduce_d(v.x, q, qinv)), pinv, q);
-            double r1 = mulmod_d<0>(__dsub_rn(u64_to_d(uu.y), reduce_d(v.y, q, qinv)), pinv, q);
-            if (add) {
+            double u0 = u64_to_d(uu.x), u1 = u64_to_d(uu.y);
+            if (EP == 4) { u0 = mulmod_dd(u0, u64_to_d(a.x), q, qinv); u1 = mulmod_dd(u1, u64_to_d(a.y), q, qinv); }
+            double r0 = mulmod_d<0>(__dsub_rn(u0, reduce_d(v.x, q, qinv)), pinv, q);
+            double r1 = mulmod_d<0>(__dsub_rn(u1, reduce_d(v.y, q, qinv)), pinv, q);
+            if (EP != 4 && add) {
                 const bool odd = sr[k & 3] & 1;
                 r0 = __dadd_rn(r0, u64_to_d(odd ? a.y : a.x));
                 r1 = __dadd_rn(r1, u64_to_d(odd ? a.x : a.y));
@@ -383,7 +388,7 @@ __global__ void __launch_bounds__(16 * ROW_CTA, 48 / ROW_CTA) ntt_inv_rows(DevTa
 }
 
 // ---- row passes of few limbs: a row by a warp -----------------------------------------------------------------------------
-// forward, EP 0 and 1 as in ntt_fwd_rows; the other operands are on their way while the row is transformed
+// forward, EP 0, 1 and 4 as in ntt_fwd_rows; the other operands are on their way while the row is transformed
 template <int EP, bool WIDE>
 __global__ void __launch_bounds__(32 * ROW_CTA, 6) ntt_fwd_wrows(DevTables c, u64 *base, LimbMap map, uint32_t fp_share, const __grid_constant__ NttEpilogue ep) {
     __shared__ __align__(16) double sm[ROW_CTA][WROW_PAD];
@@ -416,17 +421,19 @@ __global__ void __launch_bounds__(32 * ROW_CTA, 6) ntt_fwd_wrows(DevTables c, u6
     const uint32_t rot = ep.group ? bz / ep.group : bz, mem = ep.group ? bz % ep.group : bz;
     const uint32_t gal = (uint32_t)(ep.multi ? ep.mgalois[rot] : ep.galois);
     const u64 *add = (ep.add_comps >> comp & 1) ? ep.add.at(ep.own ? bz : mem) + (((size_t)comp * ep.level + i) << c.log_n) : nullptr;
-    const u64 *acc = ep.accumulate ? ep.acc.at(bz) + (((size_t)comp * ep.level + i) << c.log_n) + p0 : nullptr;
+    const u64 *acc = ep.accumulate ? ep.acc.at(bz) + (((size_t)comp * (ep.acc_pitch ? ep.acc_pitch : ep.level) + i) << c.log_n) + p0 : nullptr;
     const uint32_t bstep = ep.tl.R ? ep.tl.R * 64 : 64;        // words from one 64-word block of the destination to the next
     u64 *dst = ep.tl.R ? const_cast<u64 *>(ep.out.base) + tiled_index(ep.tl.R, c.N, ep.tl.row0 + rot * ep.rot_rows + (ep.group ? mem : bz) * ep.tl.row_stride + comp, i, row * 256) + 2 * t
                        : const_cast<u64 *>(ep.group ? ep.out.base + rot * ep.rot_stride + mem * ep.out.stride : ep.out.at(bz)) + (((size_t)comp * ep.level + i) << c.log_n) + p0;
     const u64 *up = ep.u.at(bz) + (((size_t)comp * ep.nt + i) << c.log_n) + p0;
+    const u64 *pp = EP == 4 ? ep.pt.at(bz) + ((size_t)i << c.log_n) + p0 : nullptr;
     ulonglong2 ua[4], aa[4];
     uint32_t sr[4];
 #pragma unroll
     for (uint32_t k = 0; k < 4; k++) {
         ua[k] = ld_pair<WIDE>(up + 64 * k);
-        if (add) {      // the permutation maps the pair onto a pair, possibly swapped
+        if (EP == 4) aa[k] = ld_pair<WIDE>(pp + 64 * k);
+        else if (add) {      // the permutation maps the pair onto a pair, possibly swapped
             sr[k] = galois_src(p0 + 64 * k, gal, c.log_n);
             aa[k] = ld_pair<WIDE>(add + (sr[k] & ~1u));
         }
@@ -438,9 +445,11 @@ __global__ void __launch_bounds__(32 * ROW_CTA, 6) ntt_fwd_wrows(DevTables c, u6
     for (uint32_t k = 0; k < 4; k++) {
         const double2 w = *reinterpret_cast<const double2 *>(sp + 72 * k);
         // |u - v| < 1.5 q, times P^-1 -> |.| < 0.9 q, plus up to two residues, reduced once
-        double r0 = mulmod_d<0>(__dsub_rn(u64_to_d(ua[k].x), w.x), pinv, q);
-        double r1 = mulmod_d<0>(__dsub_rn(u64_to_d(ua[k].y), w.y), pinv, q);
-        if (add) {
+        double u0 = u64_to_d(ua[k].x), u1 = u64_to_d(ua[k].y);
+        if (EP == 4) { u0 = mulmod_dd(u0, u64_to_d(aa[k].x), q, qinv); u1 = mulmod_dd(u1, u64_to_d(aa[k].y), q, qinv); }
+        double r0 = mulmod_d<0>(__dsub_rn(u0, w.x), pinv, q);
+        double r1 = mulmod_d<0>(__dsub_rn(u1, w.y), pinv, q);
+        if (EP != 4 && add) {
             const bool odd = sr[k] & 1;
             r0 = __dadd_rn(r0, u64_to_d(odd ? aa[k].y : aa[k].x));
             r1 = __dadd_rn(r1, u64_to_d(odd ? aa[k].x : aa[k].y));
@@ -454,8 +463,8 @@ __global__ void __launch_bounds__(32 * ROW_CTA, 6) ntt_fwd_wrows(DevTables c, u6
     }
 }
 
-// inverse; src as in ntt_inv_rows
-template <bool WIDE>
+// inverse; src as in ntt_inv_rows, MUL: times src.mul
+template <bool WIDE, bool MUL>
 __global__ void __launch_bounds__(32 * ROW_CTA, 8) ntt_inv_wrows(DevTables c, u64 *base, LimbMap map, uint32_t fp_share, const __grid_constant__ NttSource src) {
     __shared__ __align__(16) double sm[ROW_CTA][WROW_PAD];
     const int prime = limb_prime(map, blockIdx.y);
@@ -470,8 +479,18 @@ __global__ void __launch_bounds__(32 * ROW_CTA, 8) ntt_inv_wrows(DevTables c, u6
     ulonglong2 w[4];
 #pragma unroll
     for (uint32_t k = 0; k < 4; k++) w[k] = ld_pair<WIDE>(gs + 2 * t + 64 * k);
+    ulonglong2 m[4];
+    if (MUL) {
+        const u64 *ms = src.mul.at(blockIdx.y / map.period) + (size_t)row * 256 + 2 * t;
 #pragma unroll
-    for (uint32_t k = 0; k < 4; k++) *reinterpret_cast<double2 *>(s + wrow_at(2 * t) + 72 * k) = make_double2(u64_to_d(w[k].x), u64_to_d(w[k].y));
+        for (uint32_t k = 0; k < 4; k++) m[k] = ld_pair<WIDE>(ms + 64 * k);
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < 4; k++) {
+        double2 x = make_double2(u64_to_d(w[k].x), u64_to_d(w[k].y));
+        if (MUL) x = make_double2(mulmod_dd(x.x, u64_to_d(m[k].x), q, qinv), mulmod_dd(x.y, u64_to_d(m[k].y), q, qinv));
+        *reinterpret_cast<double2 *>(s + wrow_at(2 * t) + 72 * k) = x;
+    }
     __syncwarp();
     wrow_inverse(v, s, t, tw, R + row, q, qinv);
 #pragma unroll
@@ -711,7 +730,7 @@ static void run_ntt(const ckks_ctx *c, u64 *base, uint32_t nlimbs_total, const L
             if (part & NTT_COLS) cols();
             if (!(part & NTT_ROWS)) continue;
             bool wide = aligned16(ep ? (const void *)nullptr : (const void *)b);
-            if (ep) wide = aligned16(ep->u) && aligned16(ep->add) && aligned16(ep->acc) && aligned16(ep->out) && (ep->rot_stride & 1) == 0;
+            if (ep) wide = aligned16(ep->u) && aligned16(ep->add) && aligned16(ep->acc) && aligned16(ep->pt) && aligned16(ep->out) && (ep->rot_stride & 1) == 0;
             NttEpilogue e = ep ? *ep : NttEpilogue{};
             e.y0 = y0;
             const int mode = ep ? ep->mode : 0;
@@ -719,22 +738,24 @@ static void run_ntt(const ckks_ctx *c, u64 *base, uint32_t nlimbs_total, const L
                                                                                       ntt_fwd_rows<3, true, 4>};
             auto *k = mode == 3 ? inner[e.beta - 1]
                     : mode == 1 ? (wide ? ntt_fwd_rows<1, true> : ntt_fwd_rows<1, false>)
+                    : mode == 4 ? (wide ? ntt_fwd_rows<4, true> : ntt_fwd_rows<4, false>)
                     : mode == 2 ? (wide ? ntt_fwd_rows<2, true> : ntt_fwd_rows<2, false>)
                                 : (wide ? ntt_fwd_rows<0, true> : ntt_fwd_rows<0, false>);
-            if (mode < 2 && few)
-                launch(mode ? (wide ? ntt_fwd_wrows<1, true> : ntt_fwd_wrows<1, false>) : (wide ? ntt_fwd_wrows<0, true> : ntt_fwd_wrows<0, false>), grid, 32 * ROW_CTA, 0, s, c->dev, b, map,
-                       share, e);
+            if ((mode < 2 || mode == 4) && few)
+                launch(mode == 4 ? (wide ? ntt_fwd_wrows<4, true> : ntt_fwd_wrows<4, false>) : mode ? (wide ? ntt_fwd_wrows<1, true> : ntt_fwd_wrows<1, false>)
+                       : (wide ? ntt_fwd_wrows<0, true> : ntt_fwd_wrows<0, false>), grid, 32 * ROW_CTA, 0, s, c->dev, b, map, share, e);
             else launch(k, grid, 16 * ROW_CTA, 0, s, c->dev, b, map, share, e);
         } else if (share > 0) {
             const NttSource none{};
-            const bool wide = src ? aligned16(src->ptr) : aligned16(b);
+            const bool wide = src ? aligned16(src->ptr) && aligned16(src->mul) : aligned16(b), mul = src && src->has_mul;
             static constexpr decltype(&ntt_inv_rows<true, 1, NttEpilogue>) inner[IP_FUSED_BETA] = {
                 ntt_inv_rows<true, 1, NttEpilogue>, ntt_inv_rows<true, 2, NttEpilogue>, ntt_inv_rows<true, 3, NttEpilogue>, ntt_inv_rows<true, 4, NttEpilogue>};
             if (!(part & NTT_ROWS)) {
             } else if (ep) {
                 launch(inner[ep->beta - 1], grid, 16 * ROW_CTA, 0, s, c->dev, b, map, share, *ep);
-            } else if (few) {
-                launch(wide ? ntt_inv_wrows<true> : ntt_inv_wrows<false>, grid, 32 * ROW_CTA, 0, s, c->dev, b, map, share, src ? sr : none);
+            } else if (few || mul) {
+                launch(mul ? (wide ? ntt_inv_wrows<true, true> : ntt_inv_wrows<false, true>) : (wide ? ntt_inv_wrows<true, false> : ntt_inv_wrows<false, false>), grid, 32 * ROW_CTA, 0, s,
+                       c->dev, b, map, share, src ? sr : none);
             } else {
                 launch(wide ? ntt_inv_rows<true> : ntt_inv_rows<false>, grid, 16 * ROW_CTA, 0, s, c->dev, b, map, share, src ? sr : none);
             }

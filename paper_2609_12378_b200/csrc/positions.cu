@@ -24,21 +24,39 @@ constexpr uint32_t THREADS = 256;
 constexpr uint32_t ROT_MAX = 256;
 struct Turns { double hi[ROT_MAX / 2], lo[ROT_MAX / 2]; };      // angle per position over pi, as an unevaluated sum
 
-// cos, sin [count][half] of position first + row.  The angle over pi is formed as a sum of two doubles and reduced exactly, so that far
-// positions lose nothing: |error| is that of sincospi and of one rounding of the reduced angle.
-__global__ void __launch_bounds__(THREADS) rotary_table_kernel(const __grid_constant__ Turns w, uint64_t first, uint64_t values, uint32_t half, double magnitude,
+// The angle over pi is formed as a sum of two doubles and reduced exactly, so that far positions lose nothing.
+__device__ __forceinline__ double2 unit(double pos, double w_hi, double w_lo) {
+    const double hi = __dmul_rn(pos, w_hi), lo = __fma_rn(pos, w_lo, __fma_rn(pos, w_hi, -hi));
+    const double r = __dsub_rn(hi, __dmul_rn(2.0, rint(__dmul_rn(0.5, hi))));
+    double s, c;
+    sincospi(__dadd_rn(r, lo), &s, &c);
+    return make_double2(c, s);
+}
+// cos, sin [count][half] of position first + row, a CTA per R^2 rows and 32 columns: R + R units per column from the functions, the others
+// as products e^(i w (base + offset)), four operations where the function takes tens.  Their error is that of two units and one product,
+// below 3 * 2^-52.  Bound by its stores from R = 16 on.
+template <uint32_t R>
+__global__ void __launch_bounds__(THREADS) rotary_table_kernel(const __grid_constant__ Turns w, uint64_t first, uint64_t count, uint32_t half, double magnitude,
                                                              double *cosv, double *sinv) {
+    __shared__ double2 base[R][32], off[R][32];
+    const uint32_t col = threadIdx.x & 31, j = blockIdx.y * 32 + col, g = threadIdx.x >> 5;
+    const uint64_t row0 = (uint64_t)blockIdx.x * (R * R);
     grid_dep_sync();
-    for (uint64_t x = (uint64_t)blockIdx.x * THREADS + threadIdx.x; x < values; x += (uint64_t)gridDim.x * THREADS) {
-        const uint64_t row = x / half;
-        const uint32_t j = (uint32_t)(x - row * half);
-        const double pos = (double)(first + row), hi = __dmul_rn(pos, w.hi[j]);
-        const double lo = __fma_rn(pos, w.lo[j], __fma_rn(pos, w.hi[j], -hi));
-        const double r = __dsub_rn(hi, __dmul_rn(2.0, rint(__dmul_rn(0.5, hi))));
-        double sv, cv;
-        sincospi(__dadd_rn(r, lo), &sv, &cv);
-        cosv[x] = __dmul_rn(cv, magnitude);
-        sinv[x] = __dmul_rn(sv, magnitude);
+    if (j < half)
+        for (uint32_t x = g; x < R; x += THREADS / 32) {
+            const double2 b = unit((double)(first + row0 + x * R), w.hi[j], w.lo[j]);
+            base[x][col] = make_double2(__dmul_rn(b.x, magnitude), __dmul_rn(b.y, magnitude));
+            off[x][col] = unit((double)x, w.hi[j], w.lo[j]);
+        }
+    __syncthreads();
+    if (j >= half) return;
+#pragma unroll 4
+    for (uint32_t x = g; x < R * R; x += THREADS / 32) {
+        if (row0 + x >= count) break;
+        const double2 b = base[x / R][col], o = off[x % R][col];
+        const size_t at = (row0 + x) * half + j;
+        cosv[at] = __fma_rn(b.x, o.x, -__dmul_rn(b.y, o.y));
+        sinv[at] = __fma_rn(b.x, o.y, __dmul_rn(b.y, o.x));
     }
 }
 
@@ -241,7 +259,7 @@ extern "C" int32_t ckks_rotary_table(ckks_ctx *c, const ckks_rotary_scaling *f, 
     if (by_turns && (!(f->original_length > 0.0) || !isfinite(f->original_length) || !(many > few) || !isfinite(many))) return CKKS_ERR_ARG;
     if ((f->rot_dim & 1) || f->rot_dim > ROT_MAX || (f->kind == CKKS_ROTARY_BASE && f->rot_dim < 4)) return CKKS_ERR_UNSUPPORTED;
     // positions are exact in doubles, and so are their products' high parts once reduced
-    if (first > (1ull << 50) || count > (1ull << 40) || first + count > (1ull << 50)) return CKKS_ERR_UNSUPPORTED;
+    if (first > (1ull << 50) || count > (1ull << 38) || first + count > (1ull << 50)) return CKKS_ERR_UNSUPPORTED;
     const double rot = f->rot_dim, theta = f->kind == CKKS_ROTARY_BASE ? f->theta * pow(f->factor, rot / (rot - 2.0)) : f->theta;
     // 1 / pi as a sum of two doubles
     const double ipi_hi = 0.318309886183790671538, ipi_lo = -1.96786766751824869e-17;
@@ -263,10 +281,14 @@ extern "C" int32_t ckks_rotary_table(ckks_ctx *c, const ckks_rotary_scaling *f, 
         w.hi[j] = a * ipi_hi;
         w.lo[j] = fma(a, ipi_hi, -w.hi[j]) + a * ipi_lo;
     }
-    const uint64_t values = count * (f->rot_dim / 2);
+    const uint32_t half = f->rot_dim / 2, cols = (half + 31) / 32;
+    const double mag = f->magnitude == 0.0 ? 1.0 : f->magnitude;
     DeviceGuard guard(c->device);
-    const uint32_t grid = (uint32_t)std::min<uint64_t>((values + THREADS - 1) / THREADS, (uint64_t)c->sms * 8);
-    launch(rotary_table_kernel, grid, THREADS, 0, (cudaStream_t)stream, w, first, values, f->rot_dim / 2, f->magnitude == 0.0 ? 1.0 : f->magnitude, cosv, sinv);
+    // larger tiles once they give every SM two CTAs; below that the call is one launch's latency either way
+    if (count / 256 * cols >= 2 * (uint64_t)c->sms)
+        launch(rotary_table_kernel<16>, dim3((uint32_t)((count + 255) / 256), cols), THREADS, 0, (cudaStream_t)stream, w, first, count, half, mag, cosv, sinv);
+    else
+        launch(rotary_table_kernel<8>, dim3((uint32_t)((count + 63) / 64), cols), THREADS, 0, (cudaStream_t)stream, w, first, count, half, mag, cosv, sinv);
     return finish(c);
 }
 

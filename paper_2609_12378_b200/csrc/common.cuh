@@ -140,7 +140,9 @@ struct TiledOut { uint32_t R = 0, row0 = 0, row_stride = 0; };
 //           x < level, else p_{x-level}; with skip_own the digit's own limbs
 //           (which never leave the evaluation domain) are skipped.
 // ---------------------------------------------------------------------------
-struct LimbMap {      // kind 2: prime = first for every limb
+// kind 2: prime = first for every limb
+// kind 3: sets of position plaintexts (SlotPositions): a period holds one of q_0 .. q_{level-1}, then some of the extended basis (first limbs each)
+struct LimbMap {
     uint32_t kind, first, period, pitch, level, L, alpha, nbeta, skip_own;
 };
 // limbs [..][period][N] contiguous, limb x of every period under prime first + x
@@ -156,16 +158,30 @@ inline LimbMap ext_map(uint32_t level, uint32_t K, uint32_t L, uint32_t alpha, u
 // limbs first .. level + K - 1 of every polynomial of the extended basis, polynomials level + K limbs apart
 inline LimbMap tail_map(uint32_t first, uint32_t level, uint32_t K, uint32_t L) { return LimbMap{1, first, level + K - first, level + K, level, L, 0, 1, 0}; }
 
+// `nrot` extended plaintexts behind one of the ciphertext primes
+inline LimbMap set_map(uint32_t level, uint32_t nrot, uint32_t K, uint32_t L) {
+    return LimbMap{3, level + K, level + nrot * (level + K), level + nrot * (level + K), level, L, nrot, 1, 0};
+}
 __host__ __device__ inline int limb_prime(const LimbMap &m, uint32_t y) {
     uint32_t x = y % m.period;
     if (m.kind == 0) return (int)(m.first + x);
     if (m.kind == 2) return (int)m.first;
+    if (m.kind == 3) {
+        if (x >= m.level) x = (x - m.level) % m.first;
+        return x < m.level ? (int)x : (int)(m.L + (x - m.level));
+    }
     if (m.skip_own) {
         uint32_t j = (y / m.period) % m.nbeta, lo = j * m.alpha, hi = lo + m.alpha < m.level ? lo + m.alpha : m.level;
         if (x >= lo && x < hi) return -1;
     }
     x += m.first;
     return x < m.level ? (int)x : (int)(m.L + (x - m.level));
+}
+// which coefficient buffer of a prologue limb y is transformed from
+__host__ __device__ inline uint32_t limb_source(const LimbMap &m, uint32_t y) {
+    if (m.kind != 3) return y / m.period;
+    const uint32_t x = y % m.period;
+    return y / m.period * (1 + m.alpha) + (x < m.level ? 0 : 1 + (x - m.level) / m.first);
 }
 // index (in limbs) of limb y from the base pointer
 __host__ __device__ inline size_t limb_index(const LimbMap &m, uint32_t y) { return (size_t)(y / m.period) * m.pitch + y % m.period; }
@@ -254,6 +270,23 @@ __device__ __forceinline__ double reduce_d(double v, double q, double qinv) {   
     const double k = __dsub_rn(__fma_rn(v, qinv, MAGIC0), MAGIC0);
     return __fma_rn(-k, q, v);
 }
+// Sums of exact 100-bit products, reduced once: as in the conversions (CONV_SIGMA) with the high part a multiple of 2^51, so that |sum| may
+// reach 2^102 = 4 q^2 and eight low parts of 2^50 stay exact.  The quotient, below 2^52, is rounded to even and off by at most one more:
+// |sum()| <= 2 q.  Four operations per product and six per sum, where a reduction of every product took seven and three.
+constexpr double SUM_SIGMA = 0x1.8p+103;
+struct ProductSum {
+    double h = SUM_SIGMA, l = 0.0;
+    __device__ __forceinline__ void add(double x, double y) {
+        const double n = __fma_rn(x, y, h);
+        l = __dadd_rn(l, __fma_rn(x, y, -__dsub_rn(n, h)));
+        h = n;
+    }
+    __device__ __forceinline__ double sum(double q, double qinv) const {
+        const double hs = __dsub_rn(h, SUM_SIGMA);
+        const double k = __dsub_rn(__fma_rn(__dadd_rn(hs, l), qinv, MAGIC1), MAGIC1);
+        return __dadd_rn(__fma_rn(-k, q, hs), l);
+    }
+};
 __device__ __forceinline__ double u64_to_d(u64 x) { return __dsub_rn(__longlong_as_double((long long)(x | 0x4330000000000000ull)), TWO52); }
 __device__ __forceinline__ u64 d_to_u64(double v) { return (u64)__double_as_longlong(__dadd_rn(v, TWO52)) & 0x000FFFFFFFFFFFFFull; }
 __device__ __forceinline__ u64 canonical_d(double v, double q) { return d_to_u64(v < 0.0 ? __dadd_rn(v, q) : v); }
@@ -542,6 +575,7 @@ struct PosArgs {
     u64 *u;
     size_t own_set, fac_set, fac_rot;
     uint32_t pitch, nrot, nb, level, inv_from;
+    uint32_t share;          // (filled in) log2 of the entries that a CTA takes for the same row
     uint8_t set[KS_MULTI];
 };
 void launch_mid_rows_pos(const ckks_ctx *c, const PosArgs &a, uint32_t beta, cudaStream_t s);
@@ -595,12 +629,12 @@ void launch_encode(const ckks_ctx *c, const double *re, const double *im, uint32
                    u64 *out, void *ws, cudaStream_t s, TiledOut tiled = TiledOut(), u64 *tiled_out = nullptr);
 // Slot values formed where the encoder reads them, plaintext b of a batch of at most SLOT_SETS sets (times 1 + POS_ROT for positions).
 constexpr uint32_t SLOT_SETS = KS_MULTI;
-// Position factors of shard ciphertexts, slot ((copy dim + d) heads + h) inner + t.  b = kind * sets + set, kind 0: the factor of a channel
+// Position factors of shard ciphertexts, slot ((copy dim + d) heads + h) inner + t.  b = set * (1 + nrot) + kind, kind 0: the factor of a channel
 // itself, 1, ..: of its partner under rotation kind - 1.  Token t of begin <= t < end takes row + (t - begin) step of the tables
 // [..][rot / 2], the others zeros.
 struct SlotPositions {
     const double *cos, *sin;
-    uint32_t dim, heads, inner, rot, interleaved, step, sets, nrot;
+    uint32_t dim, heads, inner, rot, interleaved, step, nrot;
     uint32_t row[SLOT_SETS], begin[SLOT_SETS], end[SLOT_SETS];
 };
 // 1.0 for the tokens begin <= t < end of a shard ciphertext
@@ -613,12 +647,11 @@ struct SlotScores {
 };
 // -weights[h] (device)
 struct SlotHeads { const double *weights; uint32_t heads, inner, copies; };
-// out: [batch][level][N], or with `special` [batch][level + K][N]; batch <= 65535 plaintexts whose coefficients are formed by
-// launch_encode_slots in ws (encode_workspace_bytes) and transformed by launch_encode_coefs, `first` plaintexts into them
+// The coefficients of `batch` <= 65535 plaintexts, formed in ws (encode_workspace_bytes), and the transform of the ones from `first` on to the limbs
+// of map (count limbs in all)
 template <class Slots>
 void launch_encode_slots(const ckks_ctx *c, const Slots &slots, uint32_t batch, double scale, void *ws, cudaStream_t s);
-void launch_encode_coefs(const ckks_ctx *c, const void *ws, uint32_t batch, uint32_t first, uint32_t count, uint32_t level, bool special, u64 *out,
-                         cudaStream_t s);
+void launch_encode_coefs(const ckks_ctx *c, const void *ws, uint32_t batch, uint32_t first, uint32_t limbs, const LimbMap &map, u64 *out, cudaStream_t s);
 // Slot vectors of generalised diagonals, [count][n] fp64, for k = k0 .. k0+count-1 of one block pair, diagonal k pre-rotated by its
 // giant step's share k - k % B.
 void launch_extract_diagonals(const ckks_ctx *c, const double *W, uint32_t d_out_total, uint32_t in0, uint32_t m_in,

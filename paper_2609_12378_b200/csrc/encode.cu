@@ -32,7 +32,7 @@ __device__ __forceinline__ double2 slot_value(const SlotArray &a, uint32_t b, ui
     return make_double2(a.re[(size_t)b * n + j], a.im ? a.im[(size_t)b * n + j] : 0.0);
 }
 __device__ __forceinline__ double2 slot_value(const SlotPositions &a, uint32_t b, uint32_t j, uint32_t) {
-    const uint32_t kind = b / a.sets, set = b % a.sets, t = j % a.inner, d = j / (a.inner * a.heads) % a.dim, half = a.rot / 2;
+    const uint32_t kind = b % (1 + a.nrot), set = b / (1 + a.nrot), t = j % a.inner, d = j / (a.inner * a.heads) % a.dim, half = a.rot / 2;
     if (t < a.begin[set] || t >= a.end[set]) return make_double2(0.0, 0.0);
     if (d >= a.rot) return make_double2(kind ? 0.0 : 1.0, 0.0);
     const uint32_t pair = a.interleaved ? d >> 1 : d % half;
@@ -201,12 +201,10 @@ template void launch_encode_slots(const ckks_ctx *, const SlotTokens &, uint32_t
 template void launch_encode_slots(const ckks_ctx *, const SlotScores &, uint32_t, double, void *, cudaStream_t);
 template void launch_encode_slots(const ckks_ctx *, const SlotHeads &, uint32_t, double, void *, cudaStream_t);
 
-void launch_encode_coefs(const ckks_ctx *c, const void *ws, uint32_t batch, uint32_t first, uint32_t count, uint32_t level, bool special, u64 *out,
-                         cudaStream_t s) {
+void launch_encode_coefs(const ckks_ctx *c, const void *ws, uint32_t batch, uint32_t first, uint32_t limbs, const LimbMap &map, u64 *out, cudaStream_t s) {
     const long long *coef = (const long long *)((const double2 *)ws + (size_t)batch * c->n) + (size_t)first * c->N;
     const NttPrologue pro{(const u64 *)coef, false, 0};
-    const uint32_t limbs = level + (special ? c->K : 0);
-    launch_ntt(c, out, count * limbs, special ? tail_map(0, level, c->K, c->L) : plain_map(0, level), false, s, nullptr, &pro);
+    launch_ntt(c, out, limbs, map, false, s, nullptr, &pro);
 }
 
 void launch_extract_diagonals(const ckks_ctx *c, const double *W, uint32_t d_out_total, uint32_t in0, uint32_t m_in,

@@ -126,111 +126,180 @@ __global__ void __launch_bounds__(32 * MID_ROWS, TERMS ? 5 : 8) mid_rows(DevTabl
 }
 
 // The same for rotations whose results are multiplied by plaintexts (PosArgs): every rotation reads the one set of digits through its own
-// permutation, its sums meet their factor S_r in registers, and the ciphertext's own term comes on top.  Bound as mid_rows is; per
-// ciphertext the factors and the own term add nrot (level + K) + 3 level limbs of reads to the digits' and keys', where products after
-// the division by P would be passes of their own over the rotated ciphertext, and take a rescale's transforms besides.
+// permutation, its sums meet their factor S_r in registers, and the ciphertext's own term comes on top.
+struct PosRow {            // a warp's place
+    uint32_t t, rl, row, R, bz, nt, x, kt, own, set;
+    double q, qinv, pq;
+    size_t limb, cc, kc;
+};
+__device__ __forceinline__ PosRow pos_row(const DevTables &c, const PosArgs &a, uint32_t beta) {
+    PosRow p;
+    p.t = threadIdx.x & 31; p.rl = threadIdx.x >> 5; p.R = c.N >> 8;
+    p.row = blockIdx.x * (MID_ROWS >> a.share) + (p.rl >> a.share);
+    p.bz = (blockIdx.y << a.share) + (p.rl & ((1u << a.share) - 1));
+    p.nt = a.level + c.K;
+    p.x = p.nt - 1 - blockIdx.z; p.kt = p.x < a.level ? p.x : c.L + (p.x - a.level);
+    p.own = p.x < a.level ? p.x / c.alpha : beta;           // the digit that has x among its own limbs
+    p.set = a.set[p.bz & (KS_MULTI - 1)];
+    p.q = c.modd[p.kt].x; p.qinv = c.modd[p.kt].y;
+    p.pq = p.x < a.level ? c.dn_p_mod_d[p.x] : 0.0;
+    p.limb = (size_t)1 << c.log_n; p.cc = a.pitch * p.limb; p.kc = c.T * p.limb;
+    return p;
+}
+// the digits' rows `srow` in shared memory, in order
+template <uint32_t BETA>
+__device__ __forceinline__ void pos_digits(const DevTables &c, const PosArgs &a, const PosRow &p, const u64 *ct, uint32_t srow, double (&sm)[BETA][MID_ROWS][WROW_PAD]) {
+#pragma unroll 1
+    for (uint32_t j = 0; j < BETA; j++) {
+        double *s = sm[j][p.rl];
+        if (j == p.own) {
+            const u64 *d = ct + p.cc + srow * 256 + 2 * p.t;
+            ulonglong2 w[4];
+#pragma unroll
+            for (uint32_t k = 0; k < 4; k++) w[k] = ld_pair<true>(d + 64 * k);
+#pragma unroll
+            for (uint32_t k = 0; k < 4; k++) *reinterpret_cast<double2 *>(s + wrow_at(2 * p.t) + 72 * k) = make_double2(u64_to_d(w[k].x), u64_to_d(w[k].y));
+            continue;
+        }
+        const double *g = reinterpret_cast<const double *>(a.ext) + (((size_t)p.bz * BETA + j) * p.nt + p.x) * p.limb + srow * 256 + p.t;
+        double v[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; k++) v[k] = g[32 * k];
+        wrow_forward(v, s, p.t, c.twd_fwd + p.kt * p.limb, p.R + srow, p.q, p.qinv);
+    }
+    __syncwarp();
+}
+// e = S_r (<digits, key>_cm + [cm = 0] P sigma_r(c0)) of both components at the words p0 + 64 k, p0 + 64 k + 1: below 1.5 q
+template <uint32_t BETA>
+__device__ __forceinline__ void pos_pair(const DevTables &c, const PosArgs &a, const PosRow &p, const u64 *ct, uint32_t r, uint32_t k,
+                                         const double (&sm)[BETA][MID_ROWS][WROW_PAD], double2 (&e)[2]) {
+    const uint32_t gal = (uint32_t)a.galois[r], p0 = p.row * 256 + 2 * p.t + 64 * k, src = galois_src(p0, gal, c.log_n), so = src & 254u;
+    const bool odd = src & 1;                // the permutation maps the pair onto a pair, possibly swapped
+    const u64 *kp = a.evk[r] + p.kt * p.limb + p0;
+    ulonglong2 kv[BETA][2], z = make_ulonglong2(0, 0);
+#pragma unroll
+    for (uint32_t j = 0; j < BETA; j++) {
+        kv[j][0] = ld_pair<true>(kp + 2 * j * p.kc);
+        kv[j][1] = ld_pair<true>(kp + (2 * j + 1) * p.kc);
+    }
+    const ulonglong2 f = ld_pair<true>(a.fac + r * a.fac_rot + p.set * a.fac_set + p.x * p.limb + p0);
+    if (p.x < a.level) z = ld_pair<true>(ct + (src & ~1u));
+    // products of the own digit and of c0 below q^2, of the other three at most below q^2 / 2: below 4 q^2 in all
+    ProductSum s00, s01, s10, s11;
+    s00.add(u64_to_d(odd ? z.y : z.x), p.pq);
+    s01.add(u64_to_d(odd ? z.x : z.y), p.pq);
+#pragma unroll
+    for (uint32_t j = 0; j < BETA; j++) {
+        const double2 d = *reinterpret_cast<const double2 *>(sm[j][p.rl] + wrow_at(so));
+        const double d0 = odd ? d.y : d.x, d1 = odd ? d.x : d.y;
+        s00.add(d0, u64_to_d(kv[j][0].x)); s01.add(d1, u64_to_d(kv[j][0].y));
+        s10.add(d0, u64_to_d(kv[j][1].x)); s11.add(d1, u64_to_d(kv[j][1].y));
+    }
+    const double f0 = u64_to_d(f.x), f1 = u64_to_d(f.y);
+    e[0] = make_double2(mulmod_pq<1>(s00.sum(p.q, p.qinv), f0, p.q, p.qinv), mulmod_pq<1>(s01.sum(p.q, p.qinv), f1, p.q, p.qinv));
+    e[1] = make_double2(mulmod_pq<1>(s10.sum(p.q, p.qinv), f0, p.q, p.qinv), mulmod_pq<1>(s11.sum(p.q, p.qinv), f1, p.q, p.qinv));
+}
+// P C c of both components there: below 0.75 q
+__device__ __forceinline__ void pos_own(const PosArgs &a, const PosRow &p, const u64 *ct, uint32_t k, double2 (&o)[2]) {
+    o[0] = o[1] = make_double2(0.0, 0.0);
+    if (p.x >= a.level) return;
+    const uint32_t p0 = p.row * 256 + 2 * p.t + 64 * k;
+    const ulonglong2 w = ld_pair<true>(a.own + p.set * a.own_set + p.x * p.limb + p0), z0 = ld_pair<true>(ct + p0), z1 = ld_pair<true>(ct + p.cc + p0);
+    const double w0 = mulmod_dd(u64_to_d(w.x), p.pq, p.q, p.qinv), w1 = mulmod_dd(u64_to_d(w.y), p.pq, p.q, p.qinv);
+    o[0] = make_double2(mulmod_dd(u64_to_d(z0.x), w0, p.q, p.qinv), mulmod_dd(u64_to_d(z0.y), w1, p.q, p.qinv));
+    o[1] = make_double2(mulmod_dd(u64_to_d(z1.x), w0, p.q, p.qinv), mulmod_dd(u64_to_d(z1.y), w1, p.q, p.qinv));
+}
+// the row's words p0 + 64 k, p0 + 64 k + 1 in v, at most half a prime -> the inverse row pass's result in g
+__device__ __forceinline__ void pos_inverse(const DevTables &c, const PosRow &p, double (&v)[8], double *s, double *g) {
+#pragma unroll
+    for (uint32_t k = 0; k < 4; k++) *reinterpret_cast<double2 *>(s + wrow_at(2 * p.t) + 72 * k) = make_double2(v[2 * k], v[2 * k + 1]);
+    __syncwarp();
+    wrow_inverse(v, s, p.t, c.twd_inv + p.kt * p.limb, p.R + p.row, p.q, p.qinv);
+#pragma unroll
+    for (uint32_t k = 0; k < 8; k++) g[p.t + 32 * k] = v[k];
+    __syncwarp();
+}
+
+// One rotation: pair by pair, nothing is held from one to the next; the pairs of a limb that is transformed back wait in their place in u
 template <uint32_t BETA>
 __global__ void __launch_bounds__(32 * MID_ROWS, 6) mid_rows_pos(DevTables c, const __grid_constant__ PosArgs a) {
     __shared__ __align__(16) double sm[BETA][MID_ROWS][WROW_PAD];
-    const uint32_t t = threadIdx.x & 31, rl = threadIdx.x >> 5, row = blockIdx.x * MID_ROWS + rl, R = c.N >> 8;
-    const uint32_t bz = blockIdx.y, nt = a.level + c.K, x = nt - 1 - blockIdx.z, kt = x < a.level ? x : c.L + (x - a.level);
-    const double q = c.modd[kt].x, qinv = c.modd[kt].y;
-    const uint32_t p0 = row * 256 + 2 * t, own = x < a.level ? x / c.alpha : BETA;       // own: the digit that has x among its own limbs
-    const size_t limb = (size_t)1 << c.log_n, cc = a.pitch * limb, kc = c.T * limb;
-    const double *tw = c.twd_fwd + kt * limb;
-    const double pq = x < a.level ? c.dn_p_mod_d[x] : 0.0;
-    double s0[8], s1[8];               // sums of words p0 + 64 k, p0 + 64 k + 1 of both components
+    const PosRow p = pos_row(c, a, BETA);
     grid_dep_sync();
-    const u64 *ct = a.c.at(bz) + x * limb;
-    const uint32_t set = a.set[bz];
-#pragma unroll 1
-    for (uint32_t r = 0; r < a.nrot; r++) {
-        const uint32_t gal = (uint32_t)a.galois[r], srow = galois_src(row << 8, gal, c.log_n) >> 8;
-#pragma unroll 1
-        for (uint32_t j = 0; j < BETA; j++) {
-            double *s = sm[j][rl];
-            if (j == own) {
-                const u64 *d = ct + cc + srow * 256 + 2 * t;
-                ulonglong2 w[4];
+    if (p.bz >= a.nb) return;
+    const u64 *ct = a.c.at(p.bz) + p.x * p.limb;
+    pos_digits<BETA>(c, a, p, ct, galois_src(p.row << 8, (uint32_t)a.galois[0], c.log_n) >> 8, sm);
+    u64 *u0 = a.u + ((size_t)p.bz * 2 * p.nt + p.x) * p.limb + p.row * 256;
+    const bool inverse = p.x >= a.inv_from;
 #pragma unroll
-                for (uint32_t k = 0; k < 4; k++) w[k] = ld_pair<true>(d + 64 * k);
+    for (uint32_t k = 0; k < 4; k++) {
+        double2 e[2], o[2];
+        pos_pair<BETA>(c, a, p, ct, 0, k, sm, e);
+        pos_own(a, p, ct, k, o);
 #pragma unroll
-                for (uint32_t k = 0; k < 4; k++) *reinterpret_cast<double2 *>(s + wrow_at(2 * t) + 72 * k) = make_double2(u64_to_d(w[k].x), u64_to_d(w[k].y));
-                continue;
-            }
-            const double *g = reinterpret_cast<const double *>(a.ext) + (((size_t)bz * BETA + j) * nt + x) * limb + srow * 256 + t;
-            double v[8];
-#pragma unroll
-            for (uint32_t k = 0; k < 8; k++) v[k] = g[32 * k];
-            wrow_forward(v, s, t, tw, R + srow, q, qinv);
+        for (uint32_t cm = 0; cm < 2; cm++) {
+            const double x = reduce_d(__dadd_rn(e[cm].x, o[cm].x), p.q, p.qinv), y = reduce_d(__dadd_rn(e[cm].y, o[cm].y), p.q, p.qinv);
+            u64 *u = u0 + cm * p.nt * p.limb + 2 * p.t + 64 * k;
+            if (inverse) *reinterpret_cast<double2 *>(u) = make_double2(x, y);
+            else st_pair<true>(u, make_ulonglong2(canonical_d(x, p.q), canonical_d(y, p.q)));
         }
-        __syncwarp();
-        const u64 *kp = a.evk[r] + kt * limb + p0, *fp = a.fac + r * a.fac_rot + set * a.fac_set + x * limb + p0;
+        asm volatile("" ::: "memory");       // one step's words at a time: the registers hold no more
+    }
+    if (!inverse) return;
+#pragma unroll 1
+    for (uint32_t cm = 0; cm < 2; cm++, u0 += p.nt * p.limb) {
+        double v[8];
 #pragma unroll
         for (uint32_t k = 0; k < 4; k++) {
-            const uint32_t sr = galois_src(p0 + 64 * k, gal, c.log_n) & 255, so = sr & ~1u;
-            const bool odd = sr & 1;             // the permutation maps the pair onto a pair, possibly swapped
-            ulonglong2 kv[BETA][2], z = make_ulonglong2(0, 0);
+            const double2 w = *reinterpret_cast<const double2 *>(u0 + 2 * p.t + 64 * k);
+            v[2 * k] = w.x; v[2 * k + 1] = w.y;
+        }
+        __syncwarp();
+        pos_inverse(c, p, v, sm[0][p.rl], reinterpret_cast<double *>(u0));
+    }
+}
+
+// Several rotations: their sums stay in registers, five CTAs per SM
+template <uint32_t BETA>
+__global__ void __launch_bounds__(32 * MID_ROWS, 5) mid_rows_pos_sum(DevTables c, const __grid_constant__ PosArgs a) {
+    __shared__ __align__(16) double sm[BETA][MID_ROWS][WROW_PAD];
+    const PosRow p = pos_row(c, a, BETA);
+    double s[2][8];
+    grid_dep_sync();
+    if (p.bz >= a.nb) return;
+    const u64 *ct = a.c.at(p.bz) + p.x * p.limb;
 #pragma unroll
-            for (uint32_t j = 0; j < BETA; j++) {
-                kv[j][0] = ld_pair<true>(kp + 2 * j * kc + 64 * k);
-                kv[j][1] = ld_pair<true>(kp + (2 * j + 1) * kc + 64 * k);
-            }
-            const ulonglong2 f = ld_pair<true>(fp + 64 * k);
-            if (x < a.level) z = ld_pair<true>(ct + srow * 256 + so);
-            double e0 = mulmod_dd(u64_to_d(odd ? z.y : z.x), pq, q, qinv), e1 = mulmod_dd(u64_to_d(odd ? z.x : z.y), pq, q, qinv), g0 = 0.0, g1 = 0.0;
+    for (uint32_t k = 0; k < 4; k++) {
+        double2 o[2];
+        pos_own(a, p, ct, k, o);
 #pragma unroll
-            for (uint32_t j = 0; j < BETA; j++) {
-                const double2 e = *reinterpret_cast<const double2 *>(sm[j][rl] + wrow_at(so));
-                const double d0 = odd ? e.y : e.x, d1 = odd ? e.x : e.y;
-                e0 = __dadd_rn(e0, mulmod_dd(d0, u64_to_d(kv[j][0].x), q, qinv));
-                e1 = __dadd_rn(e1, mulmod_dd(d1, u64_to_d(kv[j][0].y), q, qinv));
-                g0 = __dadd_rn(g0, mulmod_dd(d0, u64_to_d(kv[j][1].x), q, qinv));
-                g1 = __dadd_rn(g1, mulmod_dd(d1, u64_to_d(kv[j][1].y), q, qinv));
+        for (uint32_t cm = 0; cm < 2; cm++) { s[cm][2 * k] = o[cm].x; s[cm][2 * k + 1] = o[cm].y; }
+    }
+#pragma unroll 1
+    for (uint32_t r = 0; r < a.nrot; r++) {
+        pos_digits<BETA>(c, a, p, ct, galois_src(p.row << 8, (uint32_t)a.galois[r], c.log_n) >> 8, sm);
+#pragma unroll
+        for (uint32_t k = 0; k < 4; k++) {
+            double2 e[2];
+            pos_pair<BETA>(c, a, p, ct, r, k, sm, e);
+#pragma unroll
+            for (uint32_t cm = 0; cm < 2; cm++) {           // below 0.75 q and 1.5 q per rotation
+                s[cm][2 * k] = __dadd_rn(s[cm][2 * k], e[cm].x);
+                s[cm][2 * k + 1] = __dadd_rn(s[cm][2 * k + 1], e[cm].y);
             }
-            // at most BETA + 1 products of 0.75 q, reduced to half a prime and multiplied: another 0.75 q
-            const double f0 = u64_to_d(f.x), f1 = u64_to_d(f.y);
-            e0 = mulmod_dd(reduce_d(e0, q, qinv), f0, q, qinv); e1 = mulmod_dd(reduce_d(e1, q, qinv), f1, q, qinv);
-            g0 = mulmod_dd(reduce_d(g0, q, qinv), f0, q, qinv); g1 = mulmod_dd(reduce_d(g1, q, qinv), f1, q, qinv);
-            if (r == 0) { s0[2 * k] = e0; s0[2 * k + 1] = e1; s1[2 * k] = g0; s1[2 * k + 1] = g1; }
-            else {
-                s0[2 * k] = __dadd_rn(s0[2 * k], e0); s0[2 * k + 1] = __dadd_rn(s0[2 * k + 1], e1);
-                s1[2 * k] = __dadd_rn(s1[2 * k], g0); s1[2 * k + 1] = __dadd_rn(s1[2 * k + 1], g1);
-            }
-            asm volatile("" ::: "memory");       // one step's words at a time: the registers hold no more
+            asm volatile("" ::: "memory");
         }
         __syncwarp();
     }
-    // P C c on the q-limbs; sums of three products are reduced to half a prime
-    const u64 *op = a.own + set * a.own_set + x * limb + p0;
-    u64 *u = a.u + ((size_t)bz * 2 * nt + x) * limb + p0;
-    const double *twi = c.twd_inv + kt * limb;
+    u64 *u = a.u + ((size_t)p.bz * 2 * p.nt + p.x) * p.limb + p.row * 256;
 #pragma unroll
-    for (uint32_t cm = 0; cm < 2; cm++, u += nt * limb) {
-        double (&v)[8] = cm ? s1 : s0;
+    for (uint32_t cm = 0; cm < 2; cm++, u += p.nt * p.limb) {
 #pragma unroll
-        for (uint32_t k = 0; k < 4; k++) {
-            if (x < a.level) {
-                const ulonglong2 z = ld_pair<true>(ct + cm * cc + p0 + 64 * k), w = ld_pair<true>(op + 64 * k);
-                v[2 * k] = __dadd_rn(v[2 * k], mulmod_dd(mulmod_dd(u64_to_d(z.x), u64_to_d(w.x), q, qinv), pq, q, qinv));
-                v[2 * k + 1] = __dadd_rn(v[2 * k + 1], mulmod_dd(mulmod_dd(u64_to_d(z.y), u64_to_d(w.y), q, qinv), pq, q, qinv));
-            }
-            v[2 * k] = reduce_d(v[2 * k], q, qinv); v[2 * k + 1] = reduce_d(v[2 * k + 1], q, qinv);
-        }
-        if (x < a.inv_from) {
+        for (uint32_t k = 0; k < 8; k++) s[cm][k] = reduce_d(s[cm][k], p.q, p.qinv);
+        if (p.x >= a.inv_from) { pos_inverse(c, p, s[cm], sm[0][p.rl], reinterpret_cast<double *>(u)); continue; }
 #pragma unroll
-            for (uint32_t k = 0; k < 4; k++) st_pair<true>(u + 64 * k, make_ulonglong2(canonical_d(v[2 * k], q), canonical_d(v[2 * k + 1], q)));
-            continue;
-        }
-        double *s = sm[0][rl];
-#pragma unroll
-        for (uint32_t k = 0; k < 4; k++) *reinterpret_cast<double2 *>(s + wrow_at(2 * t) + 72 * k) = make_double2(v[2 * k], v[2 * k + 1]);
-        __syncwarp();
-        wrow_inverse(v, s, t, twi, R + row, q, qinv);
-        double *g = reinterpret_cast<double *>(u) - t;
-#pragma unroll
-        for (uint32_t k = 0; k < 8; k++) g[32 * k] = v[k];
-        __syncwarp();
+        for (uint32_t k = 0; k < 4; k++)
+            st_pair<true>(u + 2 * p.t + 64 * k, make_ulonglong2(canonical_d(s[cm][2 * k], p.q), canonical_d(s[cm][2 * k + 1], p.q)));
     }
 }
 
@@ -238,8 +307,12 @@ __global__ void __launch_bounds__(32 * MID_ROWS, 6) mid_rows_pos(DevTables c, co
 
 void launch_mid_rows_pos(const ckks_ctx *c, const PosArgs &a, uint32_t beta, cudaStream_t s) {
     using K = decltype(&mid_rows_pos<1>);
-    static constexpr K k[IP_FUSED_BETA] = {mid_rows_pos<1>, mid_rows_pos<2>, mid_rows_pos<3>, mid_rows_pos<4>};
-    launch(k[beta - 1], dim3((c->N >> 8) / MID_ROWS, a.nb, a.level + c->K), 32 * MID_ROWS, 0, s, c->dev, a);
+    static constexpr K one[IP_FUSED_BETA] = {mid_rows_pos<1>, mid_rows_pos<2>, mid_rows_pos<3>, mid_rows_pos<4>};
+    static constexpr K sum[IP_FUSED_BETA] = {mid_rows_pos_sum<1>, mid_rows_pos_sum<2>, mid_rows_pos_sum<3>, mid_rows_pos_sum<4>};
+    PosArgs b = a;
+    b.share = a.nrot > 1 ? 0 : a.nb >= 4 ? 2 : a.nb >= 2 ? 1 : 0;
+    const uint32_t e = 1u << b.share;
+    launch((a.nrot > 1 ? sum : one)[beta - 1], dim3((c->N >> 8) / (MID_ROWS >> b.share), (a.nb + e - 1) / e, a.level + c->K), 32 * MID_ROWS, 0, s, c->dev, b);
 }
 void launch_mid_rows(const ckks_ctx *c, const MidArgs &a, uint32_t beta, cudaStream_t s) {
     using K = decltype(&mid_rows<1, false>);

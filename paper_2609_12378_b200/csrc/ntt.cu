@@ -67,7 +67,8 @@ __global__ void __launch_bounds__(ColShape<LOGR>::THREADS, 1024 / ColShape<LOGR>
     const double *tw = c.twd_fwd + ((size_t)prime << c.log_n);
     const uint32_t cc = threadIdx.x % S::COLS, r = threadIdx.x / S::COLS;
     u64 *g = base + (limb_index(map, blockIdx.y) << c.log_n) + blockIdx.x * S::COLS + cc;
-    const u64 *gs = SRC == SRC_LIMBS || SRC == SRC_DOUBLES ? g : src + ((size_t)(blockIdx.y / map.period) << c.log_n) + blockIdx.x * S::COLS + cc;
+    const u64 *gs = SRC == SRC_LIMBS || SRC == SRC_DOUBLES ? g
+                  : src + ((size_t)(SRC == SRC_COEFS ? limb_source(map, blockIdx.y) : blockIdx.y / map.period) << c.log_n) + blockIdx.x * S::COLS + cc;
     constexpr uint32_t RS = S::R / S::E;          // rows between a thread's registers in the first group
     double x[S::E];
     if (SH) stage_tw<S::R>(stw, tw);
@@ -707,7 +708,7 @@ static void run_ntt(const ckks_ctx *c, u64 *base, uint32_t nlimbs_total, const L
         u64 *b = base + (limb_index(map, y0) << c->log_n);
         NttPrologue pr;
         if (pro) pr = *pro;
-        if (pr.src) { pr.src += (size_t)(y0 / map.period) << c->log_n; }
+        if (pr.src) { pr.src += (size_t)limb_source(map, y0) << c->log_n; }
         NttSource sr;
         if (src) { sr = *src; if (!sr.ptr.n) sr.ptr.base += (size_t)(y0 / map.period) * sr.ptr.stride; }
         auto cols = [&]() {

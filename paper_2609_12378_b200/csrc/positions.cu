@@ -165,11 +165,12 @@ void rotate_items(ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, s
     const size_t N = c->N;
     const uint32_t nt = level + c->K, beta = (level + c->alpha - 1) / c->alpha, m = std::min((uint32_t)items.size(), KS_MULTI);
     const double scale = (double)c->mod[level - 1];
-    u64 *own = (u64 *)ws, *fac = own + (size_t)m * level * N;
-    void *rest = (char *)ws + align256((size_t)m * (level + p.nrot * (size_t)nt) * N * sizeof(u64));
+    const LimbMap map = set_map(level, p.nrot, c->K, c->L);        // a set: C, then the S_r
+    u64 *pts = (u64 *)ws;
+    void *rest = (char *)ws + align256((size_t)m * map.period * N * sizeof(u64));
     for (uint32_t s0 = 0; s0 < sets.size(); s0 += SLOT_SETS) {
         const uint32_t ns = std::min(SLOT_SETS, (uint32_t)sets.size() - s0);
-        SlotPositions slots{cosv, sinv, d->dim, d->heads, d->token_inner, d->rot_dim, d->layout == CKKS_ROTARY_INTERLEAVED, d->row_step, ns, p.nrot, {}, {}, {}};
+        SlotPositions slots{cosv, sinv, d->dim, d->heads, d->token_inner, d->rot_dim, d->layout == CKKS_ROTARY_INTERLEAVED, d->row_step, p.nrot, {}, {}, {}};
         std::vector<std::pair<uint32_t, uint32_t>> todo;               // (item, set)
         for (uint32_t k = 0; k < ns; k++) {
             const Item &it = items[sets[s0 + k][0]];
@@ -178,8 +179,7 @@ void rotate_items(ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, s
         }
         const uint32_t batch = ns * (1 + p.nrot);
         launch_encode_slots(c, slots, batch, scale, rest, s);
-        launch_encode_coefs(c, rest, batch, 0, ns, level, false, own, s);
-        launch_encode_coefs(c, rest, batch, ns, ns * p.nrot, level, true, fac, s);
+        launch_encode_coefs(c, rest, batch, 0, ns * map.period, map, pts, s);
         for (size_t i0 = 0; i0 < todo.size(); i0 += KS_MULTI) {
             const uint32_t nb = (uint32_t)std::min<size_t>(KS_MULTI, todo.size() - i0);
             KsWorkspace w = ks_carve(c, level, rest, nb);
@@ -197,10 +197,10 @@ void rotate_items(ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, s
                 const ckks_evk *k = find_key(c, keys, nkeys, p.rots[r]);
                 a.evk[r] = (const u64 *)k->data; a.galois[r] = k->galois;
             }
-            w.mid = ks_mid(c, level, w, c1, a.evk, p.nrot) && aligned16(a.c) && aligned16(own) && aligned16(fac);
+            w.mid = ks_mid(c, level, w, c1, a.evk, p.nrot) && aligned16(a.c) && aligned16(pts);
             ks_modup(c, c1, level, w, s, nb);
-            a.ext = w.ext; a.u = w.u; a.own = own; a.fac = fac;
-            a.own_set = (size_t)level * N; a.fac_set = (size_t)nt * N; a.fac_rot = ns * (size_t)nt * N;
+            a.ext = w.ext; a.u = w.u; a.own = pts; a.fac = pts + (size_t)level * N;
+            a.own_set = a.fac_set = map.period * N; a.fac_rot = (size_t)nt * N;
             a.pitch = pitch; a.nrot = p.nrot; a.nb = nb; a.level = level; a.inv_from = level - 1;
             if (w.mid) launch_mid_rows_pos(c, a, beta, s);
             else launch(positions_inner, dim3(c->N / THREADS, nb, nt), THREADS, 0, s, c->dev, a);
@@ -237,7 +237,7 @@ void append_items(ckks_ctx *c, uint32_t token_inner, const std::vector<Item> &it
             pr.in.p[i] = it.in; pr.acc.p[i] = it.acc; pr.out.p[i] = it.out;
         }
         launch_encode_slots(c, slots, nb, (double)c->mod[level - 1], rest, s);
-        launch_encode_coefs(c, rest, nb, 0, nb, level, false, pts, s);
+        launch_encode_coefs(c, rest, nb, 0, nb * level, plain_map(0, level), pts, s);
         launch_plain_rescale(c, pr, (u64 *)rest, s, nb);
     }
 }

@@ -623,6 +623,14 @@ class Context:
         return [self._cut(o, c) for o, c in zip(outs, oa)]
 
     # ------------------------------------------- masks, differences, positions, cache
+    def _need(self, size: str, desc: tuple, make, *args) -> int:
+        """Bytes that the library function `size` gives for a descriptor and the arguments behind it: fixed for a context, so asked for once."""
+        key = (size, desc, args)
+        n = self._ws_bytes.get(key)
+        if n is None:
+            n = self._ws_bytes[key] = int(getattr(load(), size)(self._h, C.byref(make(*desc)), *args))
+        return n
+
     def _evks(self, keys):
         return (CEvk * max(1, len(keys)))(*[CEvk(_dev_u64(x.data).data_ptr(), x.galois) for x in keys])
 
@@ -630,35 +638,38 @@ class Context:
     def _mask(tokens, causal, key_begin, key_end, window, query_offset):
         return CAttnMask(int(bool(causal)), key_begin, tokens if key_end is None else key_end, window, query_offset)
 
-    def _results(self, outs, count, level):
-        """Result ciphertexts at `level`: the caller's (checked) or fresh ones."""
-        if outs is None:
-            return [self.empty_ct(level) for _ in range(count)]
-        if len(outs) != count or any(tuple(o.data.shape) != (2, level, self.N) for o in outs):
-            raise ValueError(f"expected {count} results of shape (2, {level}, {self.N})")
-        return outs
+    def _ct2(self, ct: Ciphertext, level: int = None) -> CCt:
+        """Descriptor of a two-component ciphertext of this ring (at `level`)."""
+        t = _dev_u64(ct.data)
+        shape = t.shape
+        if len(shape) != 3 or shape[0] != 2 or shape[2] != self.N or (level is not None and shape[1] != level):
+            raise ValueError(f"expected a ciphertext of shape (2, {'level' if level is None else level}, {self.N}), got {tuple(shape)}")
+        return CCt(t.data_ptr(), shape[1], 2, ct.scale)
 
-    def _of_ring(self, *lists):
-        """Every ciphertext of the lists has two components and this ring's degree."""
-        for cts in lists:
-            for x in cts:
-                if x.data.dim() != 3 or x.data.shape[0] != 2 or x.data.shape[2] != self.N:
-                    raise ValueError(f"expected ciphertexts of shape (2, level, {self.N})")
+    def _ct2s(self, cts):
+        return (CCt * len(cts))(*[self._ct2(x) for x in cts])
+
+    def _results(self, outs, count, level):
+        """Result ciphertexts at `level`, the caller's or fresh ones, and their descriptors."""
+        if outs is None:
+            outs = [self.empty_ct(level) for _ in range(count)]
+        if len(outs) != count:
+            raise ValueError(f"expected {count} results")
+        return outs, (CCt * count)(*[self._ct2(o, level) for o in outs])
 
     def attention_mask(self, cts, tokens, heads, diag_block, token_inner: int = 1, causal: bool = False, key_begin: int = 0, key_end: int = None,
                        window: int = 0, query_offset: int = 0, outs=None, ws: torch.Tensor = None, stream=None):
         """Score-map ciphertexts (one per group) with the slots of unseen key tokens set to 0, one level down: key tokens outside
         [key_begin, key_end), past the query's position i + query_offset if causal, `window` or more positions before it if window > 0."""
-        d = CAttnDesc(tokens, heads, diag_block, 1, token_inner)
+        shape = (tokens, heads, diag_block, 1, token_inner)
+        d = CAttnDesc(*shape)
         m = self._mask(tokens, causal, key_begin, key_end, window, query_offset)
         if diag_block < 1 or len(cts) != tokens // diag_block:
             raise ValueError("expected one ciphertext per group of diag_block diagonals")
-        self._of_ring(cts)
-        level = cts[0].level
-        need = int(load().ckks_attention_mask_workspace_bytes(self._h, C.byref(d), level))
-        ws = self.workspace(need) if ws is None else ws
-        outs = self._results(outs, len(cts), max(level - 1, 1))
-        ia, oa = (CCt * len(cts))(*[_cct(x) for x in cts]), (CCt * len(cts))(*[_cct(x) for x in outs])
+        ia = self._ct2s(cts)
+        level = ia[0].level
+        ws = self.workspace(self._need("ckks_attention_mask_workspace_bytes", shape, CAttnDesc, level)) if ws is None else ws
+        outs, oa = self._results(outs, len(cts), max(level - 1, 1))
         self._check(_lib.ckks_attention_mask(self._h, C.byref(d), C.byref(m), ia, oa, ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
         for o, c in zip(outs, oa):
             o.scale = c.scale
@@ -672,15 +683,14 @@ class Context:
     def attention_difference(self, a, b, weights: torch.Tensor, tokens, heads, diag_block, token_inner: int = 1, outs=None, ws: torch.Tensor = None,
                              stream=None):
         """a[g] - weights[head] b[g] for the groups of two score maps, one level down.  weights: float64 [heads] on the device."""
-        d = CAttnDesc(tokens, heads, diag_block, 1, token_inner)
+        shape = (tokens, heads, diag_block, 1, token_inner)
+        d = CAttnDesc(*shape)
         if diag_block < 1 or len(a) != tokens // diag_block or len(b) != len(a):
             raise ValueError("expected one ciphertext per group of diag_block diagonals")
-        self._of_ring(a, b)
-        level = a[0].level
-        need = int(load().ckks_attention_difference_workspace_bytes(self._h, C.byref(d), level))
-        ws = self.workspace(need) if ws is None else ws
-        outs = self._results(outs, len(a), max(level - 1, 1))
-        aa, ba, oa = ((CCt * len(a))(*[_cct(x) for x in v]) for v in (a, b, outs))
+        aa, ba = self._ct2s(a), self._ct2s(b)
+        level = aa[0].level
+        ws = self.workspace(self._need("ckks_attention_difference_workspace_bytes", shape, CAttnDesc, level)) if ws is None else ws
+        outs, oa = self._results(outs, len(a), max(level - 1, 1))
         self._check(_lib.ckks_attention_difference(self._h, C.byref(d), aa, ba, self._weights(weights, heads), oa, ws.data_ptr(), ws.numel(),
                                                    _stream_ptr(stream)))
         for o, c in zip(outs, oa):
@@ -695,14 +705,13 @@ class Context:
         m = self._mask(tokens, causal, key_begin, key_end, window, query_offset)
         if diag_block < 1 or len(cts) != tokens // diag_block:
             raise ValueError("expected one ciphertext per group of diag_block diagonals")
-        self._of_ring(cts)
-        level = cts[0].level
+        ia = self._ct2s(cts)
+        level = ia[0].level
         need = int(load().ckks_softmax_rows_workspace_bytes(self._h, C.byref(d), C.byref(sd), level))
         if need == 0:
             raise CkksError(ERR_ARG)
         ws = self.workspace(need)
-        outs = [self.empty_ct(level) for _ in cts]
-        ia, oa = ((CCt * len(cts))(*[_cct(x) for x in v]) for v in (cts, outs))
+        outs, oa = self._results(None, len(cts), level)
         ck = CEvk(_dev_u64(rlk.data).data_ptr(), 0)
         self._check(_lib.ckks_softmax_rows_masked(self._h, C.byref(d), C.byref(sd), C.byref(m), ia, C.byref(ck), self._evks(keys), len(keys), oa,
                                                   ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
@@ -730,16 +739,14 @@ class Context:
         dim, level = len(qs[0]), qs[0][0].level
         if any(len(x) != dim for x in (*qs, *ks)):
             raise ValueError("expected one query and one key operand per channel")
-        self._of_ring(*qs, *ks, v)
         L = load()
         size = L.ckks_attention_differential_workspace_bytes if weights is not None else L.ckks_attention_masked_workspace_bytes
         need = int(size(self._h, C.byref(d), C.byref(sd), level, dim))
         if need == 0:
             raise CkksError(ERR_ARG)
         ws = self.workspace(need) if ws is None else ws
-        outs = [self.empty_ct(level - 1) for _ in v]
-        qa, ka = ([(CCt * dim)(*[_cct(x) for x in cts]) for cts in side] for side in (qs, ks))
-        va, oa = ((CCt * len(v))(*[_cct(x) for x in cts]) for cts in (v, outs))
+        qa, ka, va = [self._ct2s(x) for x in qs], [self._ct2s(x) for x in ks], self._ct2s(v)
+        outs, oa = self._results(None, len(v), max(level - 1, 1))
         ck = CEvk(_dev_u64(rlk.data).data_ptr(), 0)
         tail = (dim, va, len(v), C.byref(ck), self._evks(keys), len(keys), oa, ws.data_ptr(), ws.numel(), _stream_ptr(stream))
         if weights is None:
@@ -763,8 +770,12 @@ class Context:
         return out
 
     @staticmethod
+    def _rotary_shape(dim, heads, token_inner, rot_dim, layout, same_position=False):
+        return dim, heads, token_inner, dim if rot_dim is None else rot_dim, ROTARY_LAYOUTS[layout], 0 if same_position else 1
+
+    @staticmethod
     def _rotary_desc(dim, heads, token_inner, rot_dim, layout, same_position=False):
-        return CRotaryDesc(dim, heads, token_inner, dim if rot_dim is None else rot_dim, ROTARY_LAYOUTS[layout], 0 if same_position else 1)
+        return CRotaryDesc(*Context._rotary_shape(dim, heads, token_inner, rot_dim, layout, same_position))
 
     def rotary_rotations(self, dim: int, heads: int, token_inner: int, rot_dim: int = None, layout: str = "half"):
         """Rotations (in slots, negative: to the right) whose keys rotary and cache_append need."""
@@ -787,15 +798,14 @@ class Context:
                layout: str = "half", same_position: bool = False, outs=None, ws: torch.Tensor = None, stream=None):
         """Position rotation of shard ciphertexts, one level down: slot t of cts[i] takes row rows[i] + t of the tables (rows[i] with
         same_position, where all slots hold one token)."""
-        d = self._rotary_desc(dim, heads, token_inner, rot_dim, layout, same_position)
+        shape = self._rotary_shape(dim, heads, token_inner, rot_dim, layout, same_position)
+        d = CRotaryDesc(*shape)
         n, level = len(cts), cts[0].level
         if len(rows) != n:
             raise ValueError("expected one table row per ciphertext")
-        self._of_ring(cts)
-        need = int(load().ckks_rotary_workspace_bytes(self._h, C.byref(d), level, n))
-        ws = self.workspace(need) if ws is None else ws
-        outs = self._results(outs, n, max(level - 1, 1))
-        ia, oa = ((CCt * n)(*[_cct(x) for x in v]) for v in (cts, outs))
+        ia = self._ct2s(cts)
+        ws = self.workspace(self._need("ckks_rotary_workspace_bytes", shape, CRotaryDesc, level, n)) if ws is None else ws
+        outs, oa = self._results(outs, n, max(level - 1, 1))
         self._check(_lib.ckks_rotary(self._h, C.byref(d), ia, (C.c_uint32 * n)(*rows), n, *self._table(cos, sin, d), self._evks(keys), len(keys), oa,
                                      ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
         for o, c in zip(outs, oa):
@@ -807,7 +817,8 @@ class Context:
         """New tokens into pages: slots [begin, end) of cts_k[i], rotated to the positions row, row + 1, .. of the tables, and of cts_v[i] are
         added to page pages[i], spans[i] = (begin, end, row).  In place unless out_k, out_v name other ciphertexts (one per page; those of
         pages that are not named are left alone).  cts_k or cts_v None: only the other side; cos, sin None: keys without positions."""
-        d = self._rotary_desc(dim, heads, token_inner, rot_dim, layout, same_position)
+        shape = self._rotary_shape(dim, heads, token_inner, rot_dim, layout, same_position)
+        d = CRotaryDesc(*shape)
         n = len(pages)
         sides, npages, level = [], None, None
         for cts, pool, out in ((cts_k, page_k, out_k), (cts_v, page_v, out_v)):
@@ -817,15 +828,18 @@ class Context:
             out = pool if out is None else out
             if len(cts) != n or len(spans) != n or len(out) != len(pool) or npages not in (None, len(pool)):
                 raise ValueError("expected one ciphertext and span per page named, and as many results as pages")
-            self._of_ring(cts, pool, out)
-            npages, level = len(pool), pool[0].level
-            if any(0 <= p < npages and out[p].level != level for p in pages):
-                raise ValueError("expected results of the pages' level")
-            sides.append(((CCt * n)(*[_cct(x) for x in cts]), (CCt * npages)(*[_cct(x) for x in pool]), (CCt * npages)(*[_cct(x) for x in out]), out))
+            npages, level = len(pool), pool[pages[0]].level if 0 <= pages[0] < len(pool) else 0
+            cp, co = (CCt * npages)(), (CCt * npages)()          # descriptors of the pages that the call names
+            for p in pages:
+                if 0 <= p < npages:
+                    one = self._ct2(pool[p])
+                    cp[p] = one
+                    co[p] = one if out is pool else self._ct2(out[p], one.level)
+            sides.append((self._ct2s(cts), cp, co, out))
         if npages is None:
             raise CkksError(ERR_ARG)
-        need = int(load().ckks_cache_append_workspace_bytes(self._h, C.byref(d), level, n))
-        ws = self.workspace(need) if ws is None else ws
+        if ws is None:
+            ws = self.workspace(self._need("ckks_cache_append_workspace_bytes", shape, CRotaryDesc, level, n))
         table = self._table(cos, sin, d) if cos is not None else (None, None, 0)
         (ik, pk, ok, _), (iv, pv, ov, _) = sides
         self._check(_lib.ckks_cache_append(self._h, C.byref(d), ik, iv, n, (C.c_uint32 * n)(*pages), (CCacheSpan * n)(*[CCacheSpan(*x) for x in spans]), pk, pv,

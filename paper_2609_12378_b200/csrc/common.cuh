@@ -158,9 +158,10 @@ inline LimbMap ext_map(uint32_t level, uint32_t K, uint32_t L, uint32_t alpha, u
 // limbs first .. level + K - 1 of every polynomial of the extended basis, polynomials level + K limbs apart
 inline LimbMap tail_map(uint32_t first, uint32_t level, uint32_t K, uint32_t L) { return LimbMap{1, first, level + K - first, level + K, level, L, 0, 1, 0}; }
 
-// `nrot` extended plaintexts behind one of the ciphertext primes
-inline LimbMap set_map(uint32_t level, uint32_t nrot, uint32_t K, uint32_t L) {
-    return LimbMap{3, level + K, level + nrot * (level + K), level + nrot * (level + K), level, L, nrot, 1, 0};
+// `nrot` extended plaintexts between one of the ciphertext primes and, with `mask`, another one (alpha: plaintexts behind the first)
+inline LimbMap set_map(uint32_t level, uint32_t nrot, bool mask, uint32_t K, uint32_t L) {
+    const uint32_t period = level + nrot * (level + K) + (mask ? level : 0);
+    return LimbMap{3, level + K, period, period, level, L, nrot + (mask ? 1 : 0), 1, 0};
 }
 __host__ __device__ inline int limb_prime(const LimbMap &m, uint32_t y) {
     uint32_t x = y % m.period;
@@ -629,12 +630,12 @@ void launch_encode(const ckks_ctx *c, const double *re, const double *im, uint32
                    u64 *out, void *ws, cudaStream_t s, TiledOut tiled = TiledOut(), u64 *tiled_out = nullptr);
 // Slot values formed where the encoder reads them, plaintext b of a batch of at most SLOT_SETS sets (times 1 + POS_ROT for positions).
 constexpr uint32_t SLOT_SETS = KS_MULTI;
-// Position factors of shard ciphertexts, slot ((copy dim + d) heads + h) inner + t.  b = set * (1 + nrot) + kind, kind 0: the factor of a channel
-// itself, 1, ..: of its partner under rotation kind - 1.  Token t of begin <= t < end takes row + (t - begin) step of the tables
+// Position factors of shard ciphertexts, slot ((copy dim + d) heads + h) inner + t.  b = set * kinds + kind, kind 0: the factor of a channel
+// itself, 1 .. nrot: of its partner under rotation kind - 1, 1 + nrot: 1.0 for every channel.  Token t of begin <= t < end takes row + (t - begin) step of the tables
 // [..][rot / 2], the others zeros.
 struct SlotPositions {
     const double *cos, *sin;
-    uint32_t dim, heads, inner, rot, interleaved, step, nrot;
+    uint32_t dim, heads, inner, rot, interleaved, step, nrot, kinds;
     uint32_t row[SLOT_SETS], begin[SLOT_SETS], end[SLOT_SETS];
 };
 // 1.0 for the tokens begin <= t < end of a shard ciphertext

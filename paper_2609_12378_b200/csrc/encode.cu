@@ -32,8 +32,9 @@ __device__ __forceinline__ double2 slot_value(const SlotArray &a, uint32_t b, ui
     return make_double2(a.re[(size_t)b * n + j], a.im ? a.im[(size_t)b * n + j] : 0.0);
 }
 __device__ __forceinline__ double2 slot_value(const SlotPositions &a, uint32_t b, uint32_t j, uint32_t) {
-    const uint32_t kind = b % (1 + a.nrot), set = b / (1 + a.nrot), t = j % a.inner, d = j / (a.inner * a.heads) % a.dim, half = a.rot / 2;
+    const uint32_t kind = b % a.kinds, set = b / a.kinds, t = j % a.inner, d = j / (a.inner * a.heads) % a.dim, half = a.rot / 2;
     if (t < a.begin[set] || t >= a.end[set]) return make_double2(0.0, 0.0);
+    if (kind > a.nrot) return make_double2(1.0, 0.0);
     if (d >= a.rot) return make_double2(kind ? 0.0 : 1.0, 0.0);
     const uint32_t pair = a.interleaved ? d >> 1 : d % half;
     const bool second = a.interleaved ? d & 1 : d >= half;

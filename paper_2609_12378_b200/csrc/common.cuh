@@ -140,9 +140,7 @@ struct TiledOut { uint32_t R = 0, row0 = 0, row_stride = 0; };
 //           x < level, else p_{x-level}; with skip_own the digit's own limbs
 //           (which never leave the evaluation domain) are skipped.
 // ---------------------------------------------------------------------------
-// kind 2: prime = first for every limb
-// kind 3: sets of position plaintexts (SlotPositions): a period holds one of q_0 .. q_{level-1}, then some of the extended basis (first limbs each)
-struct LimbMap {
+struct LimbMap {      // kind 2: prime = first for every limb
     uint32_t kind, first, period, pitch, level, L, alpha, nbeta, skip_own;
 };
 // limbs [..][period][N] contiguous, limb x of every period under prime first + x
@@ -158,31 +156,24 @@ inline LimbMap ext_map(uint32_t level, uint32_t K, uint32_t L, uint32_t alpha, u
 // limbs first .. level + K - 1 of every polynomial of the extended basis, polynomials level + K limbs apart
 inline LimbMap tail_map(uint32_t first, uint32_t level, uint32_t K, uint32_t L) { return LimbMap{1, first, level + K - first, level + K, level, L, 0, 1, 0}; }
 
-// `nrot` extended plaintexts between one of the ciphertext primes and, with `mask`, another one (alpha: plaintexts behind the first)
-inline LimbMap set_map(uint32_t level, uint32_t nrot, bool mask, uint32_t K, uint32_t L) {
-    const uint32_t period = level + nrot * (level + K) + (mask ? level : 0);
-    return LimbMap{3, level + K, period, period, level, L, nrot + (mask ? 1 : 0), 1, 0};
+// sets of position plaintexts (SlotPositions), `kinds` to a set and each in the extended basis; the first and those behind the `nrot` next ones
+// need no special limbs, which the transforms of a prologue with `sets` leave out (a test in limb_prime would cost every transform of a few limbs
+// 0.2 us per pass)
+inline LimbMap set_map(uint32_t level, uint32_t nrot, uint32_t kinds, uint32_t K, uint32_t L) { return LimbMap{1, 0, level + K, level + K, level, L, nrot, kinds, 0}; }
+__host__ __device__ inline bool set_skips(const LimbMap &m, uint32_t y) {
+    const uint32_t j = (y / m.period) % m.nbeta;
+    return (j == 0 || j > m.alpha) && y % m.period >= m.level;
 }
 __host__ __device__ inline int limb_prime(const LimbMap &m, uint32_t y) {
     uint32_t x = y % m.period;
     if (m.kind == 0) return (int)(m.first + x);
     if (m.kind == 2) return (int)m.first;
-    if (m.kind == 3) {
-        if (x >= m.level) x = (x - m.level) % m.first;
-        return x < m.level ? (int)x : (int)(m.L + (x - m.level));
-    }
     if (m.skip_own) {
         uint32_t j = (y / m.period) % m.nbeta, lo = j * m.alpha, hi = lo + m.alpha < m.level ? lo + m.alpha : m.level;
         if (x >= lo && x < hi) return -1;
     }
     x += m.first;
     return x < m.level ? (int)x : (int)(m.L + (x - m.level));
-}
-// which coefficient buffer of a prologue limb y is transformed from
-__host__ __device__ inline uint32_t limb_source(const LimbMap &m, uint32_t y) {
-    if (m.kind != 3) return y / m.period;
-    const uint32_t x = y % m.period;
-    return y / m.period * (1 + m.alpha) + (x < m.level ? 0 : 1 + (x - m.level) / m.first);
 }
 // index (in limbs) of limb y from the base pointer
 __host__ __device__ inline size_t limb_index(const LimbMap &m, uint32_t y) { return (size_t)(y / m.period) * m.pitch + y % m.period; }
@@ -401,7 +392,7 @@ inline bool aligned16(const Ptrs &p) {
 //           map's periods are the entries' components)
 //   mode 2: the transform's own result is stored, but into a tiled buffer (out.base): limb y = b * level + i becomes row
 //           tl.row0 + b * tl.row_stride, limb i
-//   mode 4: as mode 1 with u[b][comp][i][p] times the plaintext pt.at(b)[i][p] in u's place
+//   mode 4: as mode 1 with u[b][comp][i][p] times the plaintext add.at(b)[i][p] in u's place (and nothing else added from add)
 constexpr uint32_t IP_FUSED_BETA = 4;
 struct NttEpilogue {
     int mode;
@@ -411,7 +402,6 @@ struct NttEpilogue {
     u64 galois;
     int accumulate;        // acc is given
     uint32_t acc_pitch;    // limbs between the components of acc (0: level)
-    Ptrs pt;               // mode 4
     TiledOut tl;
     int multi;             // batch entry b adds through mgalois[b]
     u64 mgalois[KS_MULTI];
@@ -427,21 +417,23 @@ struct NttEpilogue {
 };
 // Prologue of the forward transform: the first pass reads one buffer [batch][N] (batch = limb index / map.period) instead of
 // `base`: signed 64-bit coefficients, or (lift) residues modulo prime src_prime whose centred representatives are meant.
-// doubles: the buffer itself, which holds signed doubles of at most half a prime (the conversions' output).
+// doubles: the buffer itself, which holds signed doubles of at most half a prime (the conversions' output).  sets: coefficients, map a set_map.
 struct NttPrologue {
     const u64 *src = nullptr;
     bool lift = false;
     uint32_t src_prime = 0;
     bool doubles = false;
+    bool sets = false;
 };
 // Source of the inverse transform: the first pass reads limb x of entry b at ptr.at(b) + x * lpitch limbs, so the transform
 // runs out of place and the input stays as it is (b = limb index / map.period, x = limb index % map.period).
-// mul (may be null): every word is multiplied by the same word of limb mul.at(b) on the way (rows by a warp only).
 struct NttSource {
     Ptrs ptr;
     uint32_t lpitch = 0;
+};
+// The same with every word multiplied by the same word of limb mul.at(b) on the way
+struct NttProduct : NttSource {
     Ptrs mul;
-    uint32_t has_mul = 0;
 };
 // alone: the chain of launches belongs to a short call of its own, which for a small ring the host bounds: fewest launches.
 // inv_scale (inverse): pairs [map.period][2] that replace {N^-1, last twiddle N^-1} for limb x of every period (device
@@ -462,6 +454,8 @@ enum { CONV_UP = 0, CONV_DOWN = 1, CONV_DOWN_RS = 2 };
 bool conv_strip_prepare(const ckks_ctx *c);
 bool conv_strip(const ckks_ctx *c, int mode, uint32_t level, uint32_t items, bool alone = false);     // alone: see launch_ntt
 void launch_conv_strip(const ckks_ctx *c, int mode, const u64 *src, u64 *dst, uint32_t level, uint32_t items, cudaStream_t s);
+// inverse transform of products (see NttProduct)
+void launch_intt_product(const ckks_ctx *c, u64 *base, uint32_t nlimbs, const LimbMap &map, cudaStream_t s, const NttProduct &src);
 void launch_ntt_int(const ckks_ctx *c, u64 *b, uint32_t ny, const LimbMap &map, bool inverse, const NttSource &src, cudaStream_t s);
 
 void launch_mul_plain_acc(const ckks_ctx *c, const u64 *const *cts, u64 *const *accs, uint32_t ncts, const u64 *pt,
@@ -652,7 +646,8 @@ struct SlotHeads { const double *weights; uint32_t heads, inner, copies; };
 // of map (count limbs in all)
 template <class Slots>
 void launch_encode_slots(const ckks_ctx *c, const Slots &slots, uint32_t batch, double scale, void *ws, cudaStream_t s);
-void launch_encode_coefs(const ckks_ctx *c, const void *ws, uint32_t batch, uint32_t first, uint32_t limbs, const LimbMap &map, u64 *out, cudaStream_t s);
+void launch_encode_coefs(const ckks_ctx *c, const void *ws, uint32_t batch, uint32_t first, uint32_t limbs, const LimbMap &map, u64 *out, cudaStream_t s,
+                         bool sets = false);
 // Slot vectors of generalised diagonals, [count][n] fp64, for k = k0 .. k0+count-1 of one block pair, diagonal k pre-rotated by its
 // giant step's share k - k % B.
 void launch_extract_diagonals(const ckks_ctx *c, const double *W, uint32_t d_out_total, uint32_t in0, uint32_t m_in,

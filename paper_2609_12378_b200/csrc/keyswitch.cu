@@ -780,18 +780,18 @@ void launch_plain_rescale(const ckks_ctx *c, const PlainRescale &a, u64 *ws, cud
     const uint32_t m = a.level - 1;
     const size_t N = c->N;
     u64 *last = ws, *tmp = ws + (size_t)nb * 2 * N;
-    NttSource src;
-    src.lpitch = a.pitch; src.has_mul = 1;
+    NttProduct src;
+    src.lpitch = a.pitch;
     src.ptr.n = src.mul.n = nb;
     for (uint32_t b = 0; b < nb; b++) {
         src.ptr.p[b] = a.in.at(b) + m * N;
         src.mul.p[b] = a.pt.at(b) + m * N;
     }
-    launch_ntt(c, last, nb * 2, same_map(m, 2), true, s, nullptr, nullptr, &src);
+    launch_intt_product(c, last, nb * 2, same_map(m, 2), s, src);
     NttPrologue pro{last, true, m};
     NttEpilogue ep{};
     ep.mode = 4;
-    ep.u = a.in; ep.pt = a.pt; ep.out = a.out;
+    ep.u = a.in; ep.add = a.pt; ep.out = a.out;
     ep.pinv = c->dev.rs_inv_d + (size_t)m * c->L;
     ep.ncomp = 2; ep.level = m; ep.nt = a.pitch; ep.galois = 1;
     if (a.add) { ep.acc = a.acc; ep.acc_pitch = a.acc_pitch; ep.accumulate = 1; }

@@ -15,6 +15,8 @@
 //   1.5 * 2^53), r = fma(-k, q, p) + e = y w - k q exactly.
 // The kernels are bound by FP64 issue (eight instructions per butterfly), so what is kept small is everything around the
 // butterflies: range reductions, conversions, and load/store instructions.
+#include <type_traits>
+
 #include "butterfly.cuh"
 
 namespace {
@@ -49,11 +51,11 @@ __device__ __forceinline__ void leave_out(uint32_t fp_share) {
 }
 
 // ---- column passes -------------------------------------------------------------------------------------------------
-enum { SRC_LIMBS = 0, SRC_COEFS = 1, SRC_LIFT = 2, SRC_DOUBLES = 3 };
+enum { SRC_LIMBS = 0, SRC_COEFS = 1, SRC_LIFT = 2, SRC_DOUBLES = 3, SRC_SETS = 4 };
 
 // forward: SRC_LIMBS in place; SRC_COEFS: signed 64-bit coefficients [batch][N], reduced modulo the limb's prime on load;
 // SRC_LIFT: one residue limb per period modulo prime src_prime, lifted to its centred representative (rescale);
-// SRC_DOUBLES in place, signed doubles of at most q / 2 instead of residues (the conversions)
+// SRC_DOUBLES in place, signed doubles of at most q / 2 instead of residues (the conversions); SRC_SETS: as SRC_COEFS, for a set_map
 template <uint32_t LOGR, int SRC>
 __global__ void __launch_bounds__(ColShape<LOGR>::THREADS, 1024 / ColShape<LOGR>::THREADS) ntt_fwd_cols(DevTables c, u64 *base, LimbMap map, uint32_t fp_share,
                                                                                                     const u64 *src, uint32_t src_prime) {
@@ -63,18 +65,18 @@ __global__ void __launch_bounds__(ColShape<LOGR>::THREADS, 1024 / ColShape<LOGR>
     __shared__ __align__(16) double stw[SH ? S::R : 2];
     const int prime = limb_prime(map, blockIdx.y);
     if (prime < 0 || (blockIdx.y & 7) >= fp_share) return leave_out(fp_share);
+    if (SRC == SRC_SETS && set_skips(map, blockIdx.y)) return;
     const double q = c.modd[prime].x, qinv = c.modd[prime].y;
     const double *tw = c.twd_fwd + ((size_t)prime << c.log_n);
     const uint32_t cc = threadIdx.x % S::COLS, r = threadIdx.x / S::COLS;
     u64 *g = base + (limb_index(map, blockIdx.y) << c.log_n) + blockIdx.x * S::COLS + cc;
-    const u64 *gs = SRC == SRC_LIMBS || SRC == SRC_DOUBLES ? g
-                  : src + ((size_t)(SRC == SRC_COEFS ? limb_source(map, blockIdx.y) : blockIdx.y / map.period) << c.log_n) + blockIdx.x * S::COLS + cc;
+    const u64 *gs = SRC == SRC_LIMBS || SRC == SRC_DOUBLES ? g : src + ((size_t)(blockIdx.y / map.period) << c.log_n) + blockIdx.x * S::COLS + cc;
     constexpr uint32_t RS = S::R / S::E;          // rows between a thread's registers in the first group
     double x[S::E];
     if (SH) stage_tw<S::R>(stw, tw);
     const double *tws = SH ? stw : tw;
     grid_dep_sync();
-    if (SRC == SRC_COEFS) {
+    if (SRC == SRC_COEFS || SRC == SRC_SETS) {
         // coefficients below 2^49 (every weight of ordinary size at the scale of a prime) are residues as they are, signed;
         // anything larger in a warp takes the integer reduction
         long long v[S::E];
@@ -169,7 +171,7 @@ __global__ void __launch_bounds__(ColShape<LOGR>::THREADS, 768 / ColShape<LOGR>:
 
 // ---- row passes (see ROW_PAD) --------------------------------------------------------------------------------------------
 // forward, EP 0: in place; 1: the tail of a ModDown or rescale, (u - NTT(conv)) c + sigma_g(add), written to its final
-// place; 2: into a tiled buffer; 3: as 1 with u formed here from BETA digits and the key; 4: as 1 with u times a plaintext.  EP 3 is bound by HBM (the key words and the
+// place; 2: into a tiled buffer; 3: as 1 with u formed here from BETA digits and the key; 4: as 1 with u times a plaintext; 5: as 0 for a set_map.  EP 3 is bound by HBM (the key words and the
 // results); one pair of words per step at 64 registers: two pairs at 96 registers and 20 warps per SM took 1750 us for 64
 // rotations, four pairs at 128 registers 1910, against 1550.
 template <int EP, bool WIDE, uint32_t BETA = 1>
@@ -179,6 +181,7 @@ __global__ void __launch_bounds__(16 * ROW_CTA, 64 / ROW_CTA) ntt_fwd_rows(DevTa
     const uint32_t yl = EP == 3 ? ((blockIdx.y >> 1) % ep.nb * 2 + (blockIdx.y & 1)) * ep.level + (blockIdx.y >> 1) / ep.nb : blockIdx.y;
     const int prime = limb_prime(map, yl);
     if (prime < 0 || (yl & 7) >= fp_share) return leave_out(fp_share);
+    if (EP == 5 && set_skips(map, yl)) return;
     const double q = c.modd[prime].x, qinv = c.modd[prime].y;
     const double *tw = c.twd_fwd + ((size_t)prime << c.log_n);
     const uint32_t t = threadIdx.x & 15, rl = threadIdx.x >> 4, row = blockIdx.x * ROW_CTA + rl, R = c.N >> 8;
@@ -263,7 +266,7 @@ __global__ void __launch_bounds__(16 * ROW_CTA, 64 / ROW_CTA) ntt_fwd_rows(DevTa
         const u64 *up = ep.u.at(bz) + (((size_t)comp * ep.nt + i) << c.log_n) + p0;
         // the other operands are fetched four pairs at a time, all in flight together (one pair per step, behind the step's
         // arithmetic, was latency bound: 332 us against 243 for 16 key switches at level 24)
-        const u64 *pp = EP == 4 ? ep.pt.at(bz) + ((size_t)i << c.log_n) + p0 : nullptr;
+        const u64 *pp = EP == 4 ? ep.add.at(bz) + ((size_t)i << c.log_n) + p0 : nullptr;
         ulonglong2 ua[4], aa[4];
         uint32_t sr[4];
 #pragma unroll
@@ -389,12 +392,13 @@ __global__ void __launch_bounds__(16 * ROW_CTA, 48 / ROW_CTA) ntt_inv_rows(DevTa
 }
 
 // ---- row passes of few limbs: a row by a warp -----------------------------------------------------------------------------
-// forward, EP 0, 1 and 4 as in ntt_fwd_rows; the other operands are on their way while the row is transformed
+// forward, EP 0, 1, 4 and 5 as in ntt_fwd_rows; the other operands are on their way while the row is transformed
 template <int EP, bool WIDE>
 __global__ void __launch_bounds__(32 * ROW_CTA, 6) ntt_fwd_wrows(DevTables c, u64 *base, LimbMap map, uint32_t fp_share, const __grid_constant__ NttEpilogue ep) {
     __shared__ __align__(16) double sm[ROW_CTA][WROW_PAD];
     const int prime = limb_prime(map, blockIdx.y);
     if (prime < 0 || (blockIdx.y & 7) >= fp_share) return leave_out(fp_share);
+    if (EP == 5 && set_skips(map, blockIdx.y)) return;
     const double q = c.modd[prime].x, qinv = c.modd[prime].y;
     const double *tw = c.twd_fwd + ((size_t)prime << c.log_n);
     const uint32_t t = threadIdx.x & 31, rl = threadIdx.x >> 5, row = blockIdx.x * ROW_CTA + rl, R = c.N >> 8;
@@ -404,7 +408,7 @@ __global__ void __launch_bounds__(32 * ROW_CTA, 6) ntt_fwd_wrows(DevTables c, u6
 #pragma unroll
     for (uint32_t k = 0; k < 8; k++) v[k] = reinterpret_cast<const double *>(g)[t + 32 * k];
     const double *sp = s + wrow_at(2 * t);                // word 2 t + 64 k is 72 k further
-    if (EP == 0) {
+    if (EP == 0 || EP == 5) {
         __syncwarp();
         wrow_forward(v, s, t, tw, R + row, q, qinv);
         __syncwarp();
@@ -427,7 +431,7 @@ __global__ void __launch_bounds__(32 * ROW_CTA, 6) ntt_fwd_wrows(DevTables c, u6
     u64 *dst = ep.tl.R ? const_cast<u64 *>(ep.out.base) + tiled_index(ep.tl.R, c.N, ep.tl.row0 + rot * ep.rot_rows + (ep.group ? mem : bz) * ep.tl.row_stride + comp, i, row * 256) + 2 * t
                        : const_cast<u64 *>(ep.group ? ep.out.base + rot * ep.rot_stride + mem * ep.out.stride : ep.out.at(bz)) + (((size_t)comp * ep.level + i) << c.log_n) + p0;
     const u64 *up = ep.u.at(bz) + (((size_t)comp * ep.nt + i) << c.log_n) + p0;
-    const u64 *pp = EP == 4 ? ep.pt.at(bz) + ((size_t)i << c.log_n) + p0 : nullptr;
+    const u64 *pp = EP == 4 ? ep.add.at(bz) + ((size_t)i << c.log_n) + p0 : nullptr;
     ulonglong2 ua[4], aa[4];
     uint32_t sr[4];
 #pragma unroll
@@ -464,9 +468,10 @@ __global__ void __launch_bounds__(32 * ROW_CTA, 6) ntt_fwd_wrows(DevTables c, u6
     }
 }
 
-// inverse; src as in ntt_inv_rows, MUL: times src.mul
-template <bool WIDE, bool MUL>
-__global__ void __launch_bounds__(32 * ROW_CTA, 8) ntt_inv_wrows(DevTables c, u64 *base, LimbMap map, uint32_t fp_share, const __grid_constant__ NttSource src) {
+// inverse; src as in ntt_inv_rows
+template <bool WIDE, class Src>
+__global__ void __launch_bounds__(32 * ROW_CTA, 8) ntt_inv_wrows(DevTables c, u64 *base, LimbMap map, uint32_t fp_share, const __grid_constant__ Src src) {
+    constexpr bool MUL = std::is_same<Src, NttProduct>::value;
     __shared__ __align__(16) double sm[ROW_CTA][WROW_PAD];
     const int prime = limb_prime(map, blockIdx.y);
     if (prime < 0 || (blockIdx.y & 7) >= fp_share) return leave_out(fp_share);
@@ -481,7 +486,7 @@ __global__ void __launch_bounds__(32 * ROW_CTA, 8) ntt_inv_wrows(DevTables c, u6
 #pragma unroll
     for (uint32_t k = 0; k < 4; k++) w[k] = ld_pair<WIDE>(gs + 2 * t + 64 * k);
     ulonglong2 m[4];
-    if (MUL) {
+    if constexpr (MUL) {
         const u64 *ms = src.mul.at(blockIdx.y / map.period) + (size_t)row * 256 + 2 * t;
 #pragma unroll
         for (uint32_t k = 0; k < 4; k++) m[k] = ld_pair<WIDE>(ms + 64 * k);
@@ -672,7 +677,7 @@ void launch_cols(const ckks_ctx *c, u64 *b, uint32_t ny, const LimbMap &map, boo
     else if (!pro) launch(ntt_fwd_cols<LOGR, SRC_LIMBS>, grid, th, 0, s, c->dev, b, map, share, (const u64 *)nullptr, 0u);
     else if (pro->doubles) launch(ntt_fwd_cols<LOGR, SRC_DOUBLES>, grid, th, 0, s, c->dev, b, map, share, (const u64 *)nullptr, 0u);
     else if (pro->lift) launch(ntt_fwd_cols<LOGR, SRC_LIFT>, grid, th, 0, s, c->dev, b, map, share, pro->src, pro->src_prime);
-    else launch(ntt_fwd_cols<LOGR, SRC_COEFS>, grid, th, 0, s, c->dev, b, map, share, pro->src, 0u);
+    else launch(pro->sets ? ntt_fwd_cols<LOGR, SRC_SETS> : ntt_fwd_cols<LOGR, SRC_COEFS>, grid, th, 0, s, c->dev, b, map, share, pro->src, 0u);
 }
 
 }  // namespace
@@ -708,7 +713,7 @@ static void run_ntt(const ckks_ctx *c, u64 *base, uint32_t nlimbs_total, const L
         u64 *b = base + (limb_index(map, y0) << c->log_n);
         NttPrologue pr;
         if (pro) pr = *pro;
-        if (pr.src) { pr.src += (size_t)limb_source(map, y0) << c->log_n; }
+        if (pr.src) { pr.src += (size_t)(y0 / map.period) << c->log_n; }
         NttSource sr;
         if (src) { sr = *src; if (!sr.ptr.n) sr.ptr.base += (size_t)(y0 / map.period) * sr.ptr.stride; }
         auto cols = [&]() {
@@ -731,32 +736,34 @@ static void run_ntt(const ckks_ctx *c, u64 *base, uint32_t nlimbs_total, const L
             if (part & NTT_COLS) cols();
             if (!(part & NTT_ROWS)) continue;
             bool wide = aligned16(ep ? (const void *)nullptr : (const void *)b);
-            if (ep) wide = aligned16(ep->u) && aligned16(ep->add) && aligned16(ep->acc) && aligned16(ep->pt) && aligned16(ep->out) && (ep->rot_stride & 1) == 0;
+            if (ep) wide = aligned16(ep->u) && aligned16(ep->add) && aligned16(ep->acc) && aligned16(ep->out) && (ep->rot_stride & 1) == 0;
             NttEpilogue e = ep ? *ep : NttEpilogue{};
             e.y0 = y0;
-            const int mode = ep ? ep->mode : 0;
+            const int mode = ep ? ep->mode : pro && pro->sets ? 5 : 0;
             static constexpr decltype(&ntt_fwd_rows<0, true>) inner[IP_FUSED_BETA] = {ntt_fwd_rows<3, true, 1>, ntt_fwd_rows<3, true, 2>, ntt_fwd_rows<3, true, 3>,
                                                                                       ntt_fwd_rows<3, true, 4>};
             auto *k = mode == 3 ? inner[e.beta - 1]
                     : mode == 1 ? (wide ? ntt_fwd_rows<1, true> : ntt_fwd_rows<1, false>)
                     : mode == 4 ? (wide ? ntt_fwd_rows<4, true> : ntt_fwd_rows<4, false>)
+                    : mode == 5 ? (wide ? ntt_fwd_rows<5, true> : ntt_fwd_rows<5, false>)
                     : mode == 2 ? (wide ? ntt_fwd_rows<2, true> : ntt_fwd_rows<2, false>)
                                 : (wide ? ntt_fwd_rows<0, true> : ntt_fwd_rows<0, false>);
-            if ((mode < 2 || mode == 4) && few)
-                launch(mode == 4 ? (wide ? ntt_fwd_wrows<4, true> : ntt_fwd_wrows<4, false>) : mode ? (wide ? ntt_fwd_wrows<1, true> : ntt_fwd_wrows<1, false>)
-                       : (wide ? ntt_fwd_wrows<0, true> : ntt_fwd_wrows<0, false>), grid, 32 * ROW_CTA, 0, s, c->dev, b, map, share, e);
+            auto *kw = mode == 1 ? (wide ? ntt_fwd_wrows<1, true> : ntt_fwd_wrows<1, false>)
+                     : mode == 4 ? (wide ? ntt_fwd_wrows<4, true> : ntt_fwd_wrows<4, false>)
+                     : mode == 5 ? (wide ? ntt_fwd_wrows<5, true> : ntt_fwd_wrows<5, false>)
+                                 : (wide ? ntt_fwd_wrows<0, true> : ntt_fwd_wrows<0, false>);
+            if (few && mode != 2 && mode != 3) launch(kw, grid, 32 * ROW_CTA, 0, s, c->dev, b, map, share, e);
             else launch(k, grid, 16 * ROW_CTA, 0, s, c->dev, b, map, share, e);
         } else if (share > 0) {
             const NttSource none{};
-            const bool wide = src ? aligned16(src->ptr) && aligned16(src->mul) : aligned16(b), mul = src && src->has_mul;
+            const bool wide = src ? aligned16(src->ptr) : aligned16(b);
             static constexpr decltype(&ntt_inv_rows<true, 1, NttEpilogue>) inner[IP_FUSED_BETA] = {
                 ntt_inv_rows<true, 1, NttEpilogue>, ntt_inv_rows<true, 2, NttEpilogue>, ntt_inv_rows<true, 3, NttEpilogue>, ntt_inv_rows<true, 4, NttEpilogue>};
             if (!(part & NTT_ROWS)) {
             } else if (ep) {
                 launch(inner[ep->beta - 1], grid, 16 * ROW_CTA, 0, s, c->dev, b, map, share, *ep);
-            } else if (few || mul) {
-                launch(mul ? (wide ? ntt_inv_wrows<true, true> : ntt_inv_wrows<false, true>) : (wide ? ntt_inv_wrows<true, false> : ntt_inv_wrows<false, false>), grid, 32 * ROW_CTA, 0, s,
-                       c->dev, b, map, share, src ? sr : none);
+            } else if (few) {
+                launch(wide ? ntt_inv_wrows<true, NttSource> : ntt_inv_wrows<false, NttSource>, grid, 32 * ROW_CTA, 0, s, c->dev, b, map, share, src ? sr : none);
             } else {
                 launch(wide ? ntt_inv_rows<true> : ntt_inv_rows<false>, grid, 16 * ROW_CTA, 0, s, c->dev, b, map, share, src ? sr : none);
             }
@@ -774,6 +781,13 @@ void launch_ntt(const ckks_ctx *c, u64 *base, uint32_t nlimbs_total, const LimbM
 void launch_ntt_part(const ckks_ctx *c, NttPart part, u64 *base, uint32_t nlimbs_total, const LimbMap &map, bool inverse, cudaStream_t s, const NttEpilogue *ep,
                      const NttPrologue *pro, const NttSource *src, const double2 *inv_scale) {
     run_ntt(c, base, nlimbs_total, map, inverse, s, ep, pro, src, inv_scale, part);
+}
+
+// a row by a warp whatever the number of limbs: they are the two dropped ones of each of at most KS_MULTI ciphertexts
+void launch_intt_product(const ckks_ctx *c, u64 *base, uint32_t nlimbs, const LimbMap &map, cudaStream_t s, const NttProduct &src) {
+    const bool wide = aligned16(src.ptr) && aligned16(src.mul);
+    launch(wide ? ntt_inv_wrows<true, NttProduct> : ntt_inv_wrows<false, NttProduct>, dim3((c->N >> 8) / ROW_CTA, nlimbs), 32 * ROW_CTA, 0, s, c->dev, base, map, 8u, src);
+    launch_ntt_part(c, NTT_COLS, base, nlimbs, map, true, s);
 }
 
 // grid: three CTAs per SM, all resident at once.  Returns the butterflies one launch performs.

@@ -140,7 +140,7 @@ const ckks_evk *find_key(const ckks_ctx *c, const ckks_evk *keys, uint32_t nkeys
 // Workspace of a pass over up to `m` sets of positions and `m` ciphertexts side by side: plaintexts, then the encoder's scratch, whose
 // place the key switches take over
 size_t rotary_bytes(const ckks_ctx *c, uint32_t level, uint32_t nrot, bool mask, uint32_t m) {
-    const size_t N = c->N * sizeof(u64), pts = (size_t)m * set_map(level, nrot, mask, c->K, c->L).period * N;
+    const size_t N = c->N * sizeof(u64), pts = (size_t)m * (1 + nrot + mask) * (level + c->K) * N;
     return align256(pts) + align256(std::max(encode_workspace_bytes(c, m * (1 + nrot + mask)), (size_t)m * ks_workspace_limbs(c, level) * N));
 }
 size_t mask_bytes(const ckks_ctx *c, uint32_t level, uint32_t m) {
@@ -170,21 +170,21 @@ void rotate_items(ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, c
     const size_t N = c->N;
     const uint32_t nt = level + c->K, beta = (level + c->alpha - 1) / c->alpha, m = std::min((uint32_t)items.size(), KS_MULTI);
     const double scale = (double)c->mod[level - 1];
-    const LimbMap map = set_map(level, p.nrot, values != nullptr, c->K, c->L);        // a set: C, the S_r, the mask
+    const uint32_t kinds = 1 + p.nrot + (values ? 1 : 0);        // a set: C, the S_r, the mask, each level + K limbs apart
     u64 *pts = (u64 *)ws;
-    void *rest = (char *)ws + align256((size_t)m * map.period * N * sizeof(u64));
+    void *rest = (char *)ws + align256((size_t)m * kinds * nt * N * sizeof(u64));
     for (uint32_t s0 = 0; s0 < sets.size(); s0 += SLOT_SETS) {
         const uint32_t ns = std::min(SLOT_SETS, (uint32_t)sets.size() - s0);
-        SlotPositions slots{cosv, sinv, d->dim, d->heads, d->token_inner, d->rot_dim, d->layout == CKKS_ROTARY_INTERLEAVED, d->row_step, p.nrot, 1 + map.alpha, {}, {}, {}};
+        SlotPositions slots{cosv, sinv, d->dim, d->heads, d->token_inner, d->rot_dim, d->layout == CKKS_ROTARY_INTERLEAVED, d->row_step, p.nrot, kinds, {}, {}, {}};
         std::vector<std::pair<uint32_t, uint32_t>> todo;               // (item, set)
         for (uint32_t k = 0; k < ns; k++) {
             const Item &it = items[sets[s0 + k][0]];
             slots.row[k] = it.row; slots.begin[k] = it.begin; slots.end[k] = it.end;
             for (uint32_t i : sets[s0 + k]) todo.emplace_back(i, k);
         }
-        const uint32_t batch = ns * slots.kinds;
+        const uint32_t batch = ns * kinds;
         launch_encode_slots(c, slots, batch, scale, rest, s);
-        launch_encode_coefs(c, rest, batch, 0, ns * map.period, map, pts, s);
+        launch_encode_coefs(c, rest, batch, 0, batch * nt, set_map(level, p.nrot, kinds, c->K, c->L), pts, s, true);
         for (size_t i0 = 0; i0 < todo.size(); i0 += KS_MULTI) {
             const uint32_t nb = (uint32_t)std::min<size_t>(KS_MULTI, todo.size() - i0);
             KsWorkspace w = ks_carve(c, level, rest, nb);
@@ -204,8 +204,8 @@ void rotate_items(ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, c
             }
             w.mid = ks_mid(c, level, w, c1, a.evk, p.nrot) && aligned16(a.c) && aligned16(pts);
             ks_modup(c, c1, level, w, s, nb);
-            a.ext = w.ext; a.u = w.u; a.own = pts; a.fac = pts + (size_t)level * N;
-            a.own_set = a.fac_set = map.period * N; a.fac_rot = (size_t)nt * N;
+            a.ext = w.ext; a.u = w.u; a.own = pts; a.fac = pts + (size_t)nt * N;
+            a.own_set = a.fac_set = (size_t)kinds * nt * N; a.fac_rot = (size_t)nt * N;
             a.pitch = pitch; a.nrot = p.nrot; a.nb = nb; a.level = level; a.inv_from = level - 1;
             if (w.mid) launch_mid_rows_pos(c, a, beta, s);
             else launch(positions_inner, dim3(c->N / THREADS, nb, nt), THREADS, 0, s, c->dev, a);
@@ -217,7 +217,7 @@ void rotate_items(ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, c
             for (uint32_t b = 0; b < nb; b++) {
                 const Item &it = (*values)[todo[i0 + b].first];
                 v.in.p[b] = it.in; v.acc.p[b] = it.acc; v.out.p[b] = it.out;
-                v.pt.p[b] = pts + (todo[i0 + b].second * (size_t)map.period + map.period - level) * N;
+                v.pt.p[b] = pts + (todo[i0 + b].second * (size_t)kinds + kinds - 1) * nt * N;
             }
             launch_plain_rescale(c, v, (u64 *)rest, s, nb);
         }

@@ -59,7 +59,7 @@ enum {
     CKKS_ERR_WORKSPACE = -5,   /* workspace missing or smaller than ckks_workspace_bytes   */
     CKKS_ERR_RANGE = -6,       /* encode: a scaled value does not fit 2^62                 */
     CKKS_ERR_UNSUPPORTED = -7, /* parameters outside what the kernels implement            */
-    CKKS_ERR_CUDA = -8,        /* a CUDA runtime call failed (see ckks_last_cuda_error)    */
+    CKKS_ERR_CUDA = -8,        /* a CUDA runtime call or a host allocation failed (see ckks_last_cuda_error) */
     CKKS_ERR_TIMEOUT = -9      /* a bounded device-side wait gave up (see ckks_device_status) */
 };
 
@@ -374,7 +374,7 @@ size_t ckks_attention_workspace_bytes(const ckks_ctx *ctx, const ckks_attn_desc 
  *     if window > 0; else 0.  Key tokens are those ckks_attention_scores pairs with the slot.  Used on exponentials: a masked slot then adds
  *     nothing to its row's sum, and a row that sees no token comes out as zeros.  key_begin = key_end masks everything.
  *   ckks_attention_difference: out[g] = a[g] - rescale(b[g] * W), W the weight of the slot's head (weights: device, `heads` doubles, read when
- *     the kernels run), a[g] without its last limb.  a and b at one level, scales within 2^-30; the result has a's scale.
+ *     the kernels run; values beyond the encoder's range set ckks_encode_range_flag), a[g] without its last limb.  a and b at one level, scales within 2^-30; the result has a's scale.
  *   ckks_softmax_rows_masked: ckks_softmax_rows with u_g = rescale(p_exp(S_g - shift) * M_g) before the first round: one level more.
  *     Masked scores have to stay in p_exp's interval like all others (an encrypted value cannot be replaced), and a row's sum may be
  *     as small as one exponential, or zero in rows without a token, which the inverse square root's polynomials have to stay finite on.

@@ -638,9 +638,14 @@ class Context:
     def _mask(tokens, causal, key_begin, key_end, window, query_offset):
         return CAttnMask(int(bool(causal)), key_begin, tokens if key_end is None else key_end, window, query_offset)
 
+    def _here(self, t: torch.Tensor):
+        if t.get_device() != self.device.index:
+            raise ValueError(f"expected a tensor on the context's device {self.device}")
+
     def _ct2(self, ct: Ciphertext, level: int = None) -> CCt:
         """Descriptor of a two-component ciphertext of this ring (at `level`)."""
         t = _dev_u64(ct.data)
+        self._here(t)
         shape = t.shape
         if len(shape) != 3 or shape[0] != 2 or shape[2] != self.N or (level is not None and shape[1] != level):
             raise ValueError(f"expected a ciphertext of shape (2, {'level' if level is None else level}, {self.N}), got {tuple(shape)}")
@@ -678,6 +683,7 @@ class Context:
     def _weights(self, weights: torch.Tensor, heads: int) -> int:
         if not (weights.is_cuda and weights.dtype == torch.float64 and weights.is_contiguous() and weights.numel() == heads):
             raise TypeError("expected a contiguous CUDA float64 tensor of one weight per head")
+        self._here(weights)
         return weights.data_ptr()
 
     def attention_difference(self, a, b, weights: torch.Tensor, tokens, heads, diag_block, token_inner: int = 1, outs=None, ws: torch.Tensor = None,
@@ -766,6 +772,7 @@ class Context:
         for t in out:
             if not (t.is_cuda and t.dtype == torch.float64 and t.is_contiguous() and tuple(t.shape) == shape):
                 raise TypeError("expected contiguous CUDA float64 tensors [count][rot_dim / 2]")
+            self._here(t)
         self._check(_lib.ckks_rotary_table(self._h, C.byref(f), first, count, out[0].data_ptr(), out[1].data_ptr(), _stream_ptr(stream)))
         return out
 
@@ -787,11 +794,11 @@ class Context:
         load().ckks_rotary_rotations(self._h, C.byref(d), buf, n)
         return list(buf)
 
-    @staticmethod
-    def _table(cos, sin, d):
+    def _table(self, cos, sin, d):
         for t in (cos, sin):
             if not (t.is_cuda and t.dtype == torch.float64 and t.is_contiguous() and t.dim() == 2 and t.shape[1] * 2 == d.rot_dim and t.shape[0] == cos.shape[0]):
                 raise TypeError("expected contiguous CUDA float64 tensors [rows][rot_dim / 2]")
+            self._here(t)
         return cos.data_ptr(), sin.data_ptr(), cos.shape[0]
 
     def rotary(self, cts, rows, cos: torch.Tensor, sin: torch.Tensor, keys, dim: int, heads: int, token_inner: int, rot_dim: int = None,

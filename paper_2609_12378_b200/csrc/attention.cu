@@ -30,6 +30,7 @@ bool pow2(uint32_t x) { return x && !(x & (x - 1)); }
 int make_attn_plan(const ckks_ctx *c, const ckks_attn_desc *d, AttnPlan &p) {
     if (!d || !d->tokens || !d->heads || !d->diag_block) return CKKS_ERR_ARG;
     if (!pow2(d->tokens) || !pow2(d->diag_block) || d->tokens % d->diag_block) return CKKS_ERR_UNSUPPORTED;
+    if (d->tokens > c->n || d->heads > c->n) return CKKS_ERR_UNSUPPORTED;          // (three factors of at most 2^15 below)
     const uint64_t block = (uint64_t)d->diag_block * d->tokens * d->heads;
     if (block > c->n || c->n % block) return CKKS_ERR_UNSUPPORTED;
     p.E = d->diag_block; p.Tk = d->tokens; p.H = d->heads; p.R = (uint32_t)(c->n / block); p.G = p.Tk / p.E;
@@ -74,11 +75,6 @@ int check_cts(const ckks_ctx *c, const ckks_ct *cts, uint32_t n, uint32_t *level
 }
 
 bool rlk_ok(const ckks_evk *rlk) { return rlk && rlk->data && rlk->galois == 0; }
-
-bool apart(const void *a, size_t na, const void *b, size_t nb) {
-    const char *x = (const char *)a, *y = (const char *)b;
-    return x + na <= y || y + nb <= x;
-}
 
 uint32_t log2_ceil(uint32_t x) { uint32_t d = 0; while ((1u << d) < x) d++; return d; }
 
@@ -262,13 +258,12 @@ static void difference_groups(const ckks_ctx *c, const AttnPlan &p, const double
 // results may not lie on inputs or on each other
 static bool results_apart(const ckks_ctx *c, uint32_t level, const ckks_ct *const *in, uint32_t nin, const ckks_ct *out, uint32_t G) {
     const size_t bi = (size_t)2 * level * c->N * sizeof(u64), bo = (size_t)2 * (level - 1) * c->N * sizeof(u64);
-    for (uint32_t g = 0; g < G; g++)
-        for (uint32_t h = 0; h < G; h++) {
-            for (uint32_t x = 0; x < nin; x++)
-                if (!apart(out[g].data, bo, in[x][h].data, bi)) return false;
-            if (g != h && !apart(out[g].data, bo, out[h].data, bo)) return false;
-        }
-    return true;
+    Buffers buffers;
+    for (uint32_t g = 0; g < G; g++) {
+        for (uint32_t x = 0; x < nin; x++) buffers.read(in[x][g].data, bi);
+        buffers.write(out[g].data, bo);
+    }
+    return buffers.apart();
 }
 
 extern "C" size_t ckks_attention_mask_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
@@ -280,25 +275,27 @@ extern "C" size_t ckks_attention_mask_workspace_bytes(const ckks_ctx *c, const c
 extern "C" int32_t ckks_attention_mask(ckks_ctx *c, const ckks_attn_desc *d, const ckks_attn_mask *m, const ckks_ct *in, ckks_ct *out, void *ws, size_t ws_bytes,
                                        void *stream) {
     if (!c || !out) return CKKS_ERR_ARG;
-    AttnPlan p;
-    int rc = make_attn_plan(c, d, p);
-    if (rc) return rc;
-    if (!mask_ok(p, m)) return CKKS_ERR_ARG;
-    uint32_t level;
-    if ((rc = check_cts(c, in, p.G, &level, false))) return rc;
-    if (level < 2) return CKKS_ERR_LEVEL;
-    for (uint32_t g = 0; g < p.G; g++)
-        if (!out[g].data) return CKKS_ERR_ARG;
-    if (!results_apart(c, level, &in, 1, out, p.G)) return CKKS_ERR_ARG;
-    if (!ws || ws_bytes < ckks_attention_mask_workspace_bytes(c, d, level)) return CKKS_ERR_WORKSPACE;
-    std::vector<const u64 *> vi;
-    std::vector<u64 *> vo;
-    for (uint32_t g = 0; g < p.G; g++) { vi.push_back((const u64 *)in[g].data); vo.push_back((u64 *)out[g].data); }
-    DeviceGuard guard(c->device);
-    mask_groups(c, p, *m, vi.data(), vo.data(), level, ws, (cudaStream_t)stream);
-    rc = finish(c);
-    for (uint32_t g = 0; g < p.G && rc == CKKS_OK; g++) { out[g].level = level - 1; out[g].ncomp = 2; out[g].scale = in[g].scale; }
-    return rc;
+    return guarded(c, [&]() -> int32_t {
+        AttnPlan p;
+        int rc = make_attn_plan(c, d, p);
+        if (rc) return rc;
+        if (!mask_ok(p, m)) return CKKS_ERR_ARG;
+        uint32_t level;
+        if ((rc = check_cts(c, in, p.G, &level, false))) return rc;
+        if (level < 2) return CKKS_ERR_LEVEL;
+        for (uint32_t g = 0; g < p.G; g++)
+            if (!out[g].data) return CKKS_ERR_ARG;
+        if (!results_apart(c, level, &in, 1, out, p.G)) return CKKS_ERR_ARG;
+        if (!ws || ws_bytes < ckks_attention_mask_workspace_bytes(c, d, level)) return CKKS_ERR_WORKSPACE;
+        std::vector<const u64 *> vi;
+        std::vector<u64 *> vo;
+        for (uint32_t g = 0; g < p.G; g++) { vi.push_back((const u64 *)in[g].data); vo.push_back((u64 *)out[g].data); }
+        DeviceGuard guard(c->device);
+        mask_groups(c, p, *m, vi.data(), vo.data(), level, ws, (cudaStream_t)stream);
+        rc = finish(c);
+        for (uint32_t g = 0; g < p.G && rc == CKKS_OK; g++) { out[g].level = level - 1; out[g].ncomp = 2; out[g].scale = in[g].scale; }
+        return rc;
+    });
 }
 
 extern "C" size_t ckks_attention_difference_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
@@ -310,24 +307,26 @@ extern "C" size_t ckks_attention_difference_workspace_bytes(const ckks_ctx *c, c
 extern "C" int32_t ckks_attention_difference(ckks_ctx *c, const ckks_attn_desc *d, const ckks_ct *x, const ckks_ct *y, const double *weights, ckks_ct *out, void *ws,
                                              size_t ws_bytes, void *stream) {
     if (!c || !out || !weights) return CKKS_ERR_ARG;
-    AttnPlan p;
-    int rc = make_attn_plan(c, d, p);
-    if (rc) return rc;
-    uint32_t level, ly;
-    if ((rc = check_cts(c, x, p.G, &level, true)) || (rc = check_cts(c, y, p.G, &ly, true))) return rc;
-    if (ly != level || level < 2) return CKKS_ERR_LEVEL;
-    for (uint32_t g = 0; g < p.G; g++) {
-        if (!out[g].data) return CKKS_ERR_ARG;
-        if (!scales_agree(x[g].scale, y[g].scale)) return CKKS_ERR_SCALE;
-    }
-    const ckks_ct *ins[2] = {x, y};
-    if (!results_apart(c, level, ins, 2, out, p.G)) return CKKS_ERR_ARG;
-    if (!ws || ws_bytes < ckks_attention_difference_workspace_bytes(c, d, level)) return CKKS_ERR_WORKSPACE;
-    DeviceGuard guard(c->device);
-    difference_groups(c, p, weights, x, y, out, level, ws, (cudaStream_t)stream);
-    rc = finish(c);
-    for (uint32_t g = 0; g < p.G && rc == CKKS_OK; g++) { out[g].level = level - 1; out[g].ncomp = 2; out[g].scale = x[g].scale; }
-    return rc;
+    return guarded(c, [&]() -> int32_t {
+        AttnPlan p;
+        int rc = make_attn_plan(c, d, p);
+        if (rc) return rc;
+        uint32_t level, ly;
+        if ((rc = check_cts(c, x, p.G, &level, true)) || (rc = check_cts(c, y, p.G, &ly, true))) return rc;
+        if (ly != level || level < 2) return CKKS_ERR_LEVEL;
+        for (uint32_t g = 0; g < p.G; g++) {
+            if (!out[g].data) return CKKS_ERR_ARG;
+            if (!scales_agree(x[g].scale, y[g].scale)) return CKKS_ERR_SCALE;
+        }
+        const ckks_ct *ins[2] = {x, y};
+        if (!results_apart(c, level, ins, 2, out, p.G)) return CKKS_ERR_ARG;
+        if (!ws || ws_bytes < ckks_attention_difference_workspace_bytes(c, d, level)) return CKKS_ERR_WORKSPACE;
+        DeviceGuard guard(c->device);
+        difference_groups(c, p, weights, x, y, out, level, ws, (cudaStream_t)stream);
+        rc = finish(c);
+        for (uint32_t g = 0; g < p.G && rc == CKKS_OK; g++) { out[g].level = level - 1; out[g].ncomp = 2; out[g].scale = x[g].scale; }
+        return rc;
+    });
 }
 
 // ---- Softmax over rows spread across the groups ---------------------------------------------------------------------
@@ -484,8 +483,8 @@ extern "C" int32_t ckks_softmax_rows(ckks_ctx *c, const ckks_attn_desc *d, const
 }
 extern "C" int32_t ckks_softmax_rows_masked(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_attn_mask *mask, const ckks_ct *in,
                                             const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
-    if (!mask) return CKKS_ERR_ARG;
-    return softmax_rows(c, d, s, mask, in, rlk, keys, nkeys, out, ws, ws_bytes, stream);
+    if (!c || !mask) return CKKS_ERR_ARG;
+    return guarded(c, [&] { return softmax_rows(c, d, s, mask, in, rlk, keys, nkeys, out, ws, ws_bytes, stream); });
 }
 
 // ---- probability x value ------------------------------------------------------------------------------------------
@@ -672,8 +671,8 @@ extern "C" size_t ckks_attention_masked_workspace_bytes(const ckks_ctx *c, const
 extern "C" int32_t ckks_attention_masked(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_attn_mask *mask, const ckks_ct *q, const ckks_ct *k,
                                          uint32_t dim, const ckks_ct *v, uint32_t dim_v, const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws,
                                          size_t ws_bytes, void *stream) {
-    if (!mask) return CKKS_ERR_ARG;
-    return attend(c, d, s, mask, nullptr, 1, &q, &k, dim, v, dim_v, rlk, keys, nkeys, out, ws, ws_bytes, stream);
+    if (!c || !mask) return CKKS_ERR_ARG;
+    return guarded(c, [&] { return attend(c, d, s, mask, nullptr, 1, &q, &k, dim, v, dim_v, rlk, keys, nkeys, out, ws, ws_bytes, stream); });
 }
 extern "C" size_t ckks_attention_differential_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, uint32_t level, uint32_t dim) {
     return maps_bytes(c, d, s, level, dim, 2);
@@ -681,9 +680,9 @@ extern "C" size_t ckks_attention_differential_workspace_bytes(const ckks_ctx *c,
 extern "C" int32_t ckks_attention_differential(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_attn_mask *mask, const double *weights,
                                                const ckks_ct *q1, const ckks_ct *k1, const ckks_ct *q2, const ckks_ct *k2, uint32_t dim, const ckks_ct *v, uint32_t dim_v,
                                                const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
-    if (!weights) return CKKS_ERR_ARG;
+    if (!c || !weights) return CKKS_ERR_ARG;
     const ckks_ct *q[2] = {q1, q2}, *k[2] = {k1, k2};
-    return attend(c, d, s, mask, weights, 2, q, k, dim, v, dim_v, rlk, keys, nkeys, out, ws, ws_bytes, stream);
+    return guarded(c, [&] { return attend(c, d, s, mask, weights, 2, q, k, dim, v, dim_v, rlk, keys, nkeys, out, ws, ws_bytes, stream); });
 }
 
 // ---- conversion between the projections' token-shard layout and the attention operands ---------------------------------

@@ -7,6 +7,7 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <exception>
 #include <string>
 #include <vector>
 
@@ -690,6 +691,33 @@ inline int finish(ckks_ctx *c) {
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) { c->cuda_error = cudaGetErrorString(e); return CKKS_ERR_CUDA; }
     return CKKS_OK;
+}
+// Buffers of a call: whether no written one shares a byte with another written or a read one
+struct Buffers {
+    struct Range { uintptr_t lo, hi; bool written; };
+    std::vector<Range> all;
+    void read(const void *p, size_t bytes) { all.push_back(Range{(uintptr_t)p, (uintptr_t)p + bytes, false}); }
+    void write(const void *p, size_t bytes) { all.push_back(Range{(uintptr_t)p, (uintptr_t)p + bytes, true}); }
+    bool apart() {
+        std::sort(all.begin(), all.end(), [](const Range &a, const Range &b) { return a.lo < b.lo; });
+        uintptr_t end = 0, end_written = 0;         // of the ranges so far
+        for (const Range &r : all) {
+            if (r.lo < (r.written ? end : end_written)) return false;
+            end = std::max(end, r.hi);
+            if (r.written) end_written = std::max(end_written, r.hi);
+        }
+        return true;
+    }
+};
+// An entry point's body: exceptions of host allocations end here
+template <class F>
+inline int32_t guarded(ckks_ctx *c, F body) {
+    try {
+        return body();
+    } catch (const std::exception &e) {
+        try { c->cuda_error = e.what(); } catch (...) {}
+        return CKKS_ERR_CUDA;
+    }
 }
 inline bool scales_agree(double a, double b) { return fabs(a - b) <= ldexp(fmax(fabs(a), fabs(b)), -30); }
 inline bool ct_ok(const ckks_ct *ct) { return ct && ct->data; }

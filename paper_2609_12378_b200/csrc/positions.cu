@@ -257,11 +257,6 @@ void append_items(ckks_ctx *c, uint32_t token_inner, const std::vector<Item> &it
     }
 }
 
-bool apart(const void *a, size_t na, const void *b, size_t nb) {
-    const char *x = (const char *)a, *y = (const char *)b;
-    return x + na <= y || y + nb <= x;
-}
-
 }  // namespace
 
 extern "C" int32_t ckks_rotary_table(ckks_ctx *c, const ckks_rotary_scaling *f, uint64_t first, uint64_t count, double *cosv, double *sinv, void *stream) {
@@ -325,31 +320,33 @@ extern "C" size_t ckks_rotary_workspace_bytes(const ckks_ctx *c, const ckks_rota
 extern "C" int32_t ckks_rotary(ckks_ctx *c, const ckks_rotary_desc *d, const ckks_ct *in, const uint32_t *rows, uint32_t n, const double *cosv, const double *sinv, uint32_t table_rows,
                                const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
     if (!c || !in || !rows || !n || !cosv || !sinv || !out) return CKKS_ERR_ARG;
-    RotaryPlan p;
-    int rc = make_plan(c, d, p);
-    if (rc) return rc;
-    for (uint32_t i = 0; i < n; i++) {
-        if (!in[i].data || in[i].ncomp != 2 || !out[i].data) return CKKS_ERR_ARG;
-        if ((uint64_t)rows[i] + (uint64_t)(d->token_inner - 1) * d->row_step >= table_rows) return CKKS_ERR_ARG;
-    }
-    const uint32_t level = in[0].level;
-    if (level < 2 || level > c->L) return CKKS_ERR_LEVEL;
-    for (uint32_t i = 1; i < n; i++)
-        if (in[i].level != level) return CKKS_ERR_LEVEL;
-    const size_t bi = (size_t)2 * level * c->N * sizeof(u64), bo = (size_t)2 * (level - 1) * c->N * sizeof(u64);
-    for (uint32_t i = 0; i < n; i++)
-        for (uint32_t j = 0; j < n; j++)
-            if (!apart(out[i].data, bo, in[j].data, bi) || (i != j && !apart(out[i].data, bo, out[j].data, bo))) return CKKS_ERR_ARG;
-    for (uint32_t r = 0; r < p.nrot; r++)
-        if (!find_key(c, keys, nkeys, p.rots[r])) return CKKS_ERR_NO_KEY;
-    if (!ws || ws_bytes < rotary_bytes(c, level, p.nrot, false, std::min(n, KS_MULTI))) return CKKS_ERR_WORKSPACE;
-    std::vector<Item> items;
-    for (uint32_t i = 0; i < n; i++) items.push_back(Item{(const u64 *)in[i].data, nullptr, (u64 *)out[i].data, rows[i], 0, d->token_inner});
-    DeviceGuard guard(c->device);
-    rotate_items(c, d, p, items, level, level, cosv, sinv, keys, nkeys, ws, (cudaStream_t)stream);
-    rc = finish(c);
-    for (uint32_t i = 0; i < n && rc == CKKS_OK; i++) { out[i].level = level - 1; out[i].ncomp = 2; out[i].scale = in[i].scale; }
-    return rc;
+    return guarded(c, [&]() -> int32_t {
+        RotaryPlan p;
+        int rc = make_plan(c, d, p);
+        if (rc) return rc;
+        for (uint32_t i = 0; i < n; i++) {
+            if (!in[i].data || in[i].ncomp != 2 || !out[i].data) return CKKS_ERR_ARG;
+            if ((uint64_t)rows[i] + (uint64_t)(d->token_inner - 1) * d->row_step >= table_rows) return CKKS_ERR_ARG;
+        }
+        const uint32_t level = in[0].level;
+        if (level < 2 || level > c->L) return CKKS_ERR_LEVEL;
+        for (uint32_t i = 1; i < n; i++)
+            if (in[i].level != level) return CKKS_ERR_LEVEL;
+        const size_t bi = (size_t)2 * level * c->N * sizeof(u64), bo = (size_t)2 * (level - 1) * c->N * sizeof(u64);
+        Buffers buffers;
+        for (uint32_t i = 0; i < n; i++) { buffers.read(in[i].data, bi); buffers.write(out[i].data, bo); }
+        if (!buffers.apart()) return CKKS_ERR_ARG;
+        for (uint32_t r = 0; r < p.nrot; r++)
+            if (!find_key(c, keys, nkeys, p.rots[r])) return CKKS_ERR_NO_KEY;
+        if (!ws || ws_bytes < rotary_bytes(c, level, p.nrot, false, std::min(n, KS_MULTI))) return CKKS_ERR_WORKSPACE;
+        std::vector<Item> items;
+        for (uint32_t i = 0; i < n; i++) items.push_back(Item{(const u64 *)in[i].data, nullptr, (u64 *)out[i].data, rows[i], 0, d->token_inner});
+        DeviceGuard guard(c->device);
+        rotate_items(c, d, p, items, level, level, cosv, sinv, keys, nkeys, ws, (cudaStream_t)stream);
+        rc = finish(c);
+        for (uint32_t i = 0; i < n && rc == CKKS_OK; i++) { out[i].level = level - 1; out[i].ncomp = 2; out[i].scale = in[i].scale; }
+        return rc;
+    });
 }
 
 extern "C" size_t ckks_cache_append_workspace_bytes(const ckks_ctx *c, const ckks_rotary_desc *d, uint32_t page_level, uint32_t n) {
@@ -364,71 +361,70 @@ extern "C" int32_t ckks_cache_append(ckks_ctx *c, const ckks_rotary_desc *d, con
                                      const double *sinv, uint32_t table_rows, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out_k, ckks_ct *out_v, void *ws, size_t ws_bytes,
                                      void *stream) {
     if (!c || !n || !pages || !spans || !npages || (!in_k && !in_v)) return CKKS_ERR_ARG;
-    if ((in_k && (!page_k || !out_k)) || (in_v && (!page_v || !out_v)) || (!cosv) != (!sinv)) return CKKS_ERR_ARG;
-    RotaryPlan p;
-    int rc = make_plan(c, d, p);
-    if (rc) return rc;
-    const bool rotated = in_k && cosv;
-    for (uint32_t i = 0; i < n; i++) {
-        if (pages[i] >= npages || spans[i].begin >= spans[i].end || spans[i].end > d->token_inner) return CKKS_ERR_ARG;
-        for (uint32_t j = 0; j < i; j++)
-            if (pages[j] == pages[i]) return CKKS_ERR_ARG;
-        if (rotated && (uint64_t)spans[i].row + (uint64_t)(spans[i].end - 1 - spans[i].begin) * d->row_step >= table_rows) return CKKS_ERR_ARG;
-    }
-    // descriptors: every side of the call on its own, then the buffers that are written against all others
-    struct Side { const ckks_ct *in, *page; ckks_ct *out; uint32_t level, pitch; };
-    std::vector<Side> sides;
-    if (in_k) sides.push_back(Side{in_k, page_k, out_k, 0, 0});
-    if (in_v) sides.push_back(Side{in_v, page_v, out_v, 0, 0});
-    uint32_t level = 0;
-    for (Side &sd : sides) {
+    return guarded(c, [&]() -> int32_t {
+        if ((in_k && (!page_k || !out_k)) || (in_v && (!page_v || !out_v)) || (!cosv) != (!sinv)) return CKKS_ERR_ARG;
+        RotaryPlan p;
+        int rc = make_plan(c, d, p);
+        if (rc) return rc;
+        const bool rotated = in_k && cosv;
+        std::vector<uint32_t> named(pages, pages + n);
+        std::sort(named.begin(), named.end());
+        if (named.back() >= npages || std::adjacent_find(named.begin(), named.end()) != named.end()) return CKKS_ERR_ARG;
         for (uint32_t i = 0; i < n; i++) {
-            const ckks_ct &x = sd.in[i], &pg = sd.page[pages[i]];
-            if (!x.data || x.ncomp != 2 || !pg.data || pg.ncomp != 2 || !sd.out[pages[i]].data) return CKKS_ERR_ARG;
+            if (spans[i].begin >= spans[i].end || spans[i].end > d->token_inner) return CKKS_ERR_ARG;
+            if (rotated && (uint64_t)spans[i].row + (uint64_t)(spans[i].end - 1 - spans[i].begin) * d->row_step >= table_rows) return CKKS_ERR_ARG;
         }
-        sd.pitch = sd.in[0].level; sd.level = sd.page[pages[0]].level;
-        if (!level) level = sd.level;
-        if (sd.level < 1 || sd.level != level || sd.pitch <= level || sd.pitch > c->L) return CKKS_ERR_LEVEL;
-        for (uint32_t i = 0; i < n; i++)
-            if (sd.in[i].level != sd.pitch || sd.page[pages[i]].level != level) return CKKS_ERR_LEVEL;
-        for (uint32_t i = 0; i < n; i++)
-            if (!scales_agree(sd.in[i].scale, sd.page[pages[i]].scale)) return CKKS_ERR_SCALE;
-    }
-    const size_t bp = (size_t)2 * level * c->N * sizeof(u64);
-    for (size_t x = 0; x < sides.size(); x++)
-        for (uint32_t i = 0; i < n; i++) {
-            const void *o = sides[x].out[pages[i]].data;
-            for (size_t y = 0; y < sides.size(); y++)
-                for (uint32_t j = 0; j < n; j++) {
-                    const Side &sd = sides[y];
-                    const bool same = x == y && i == j;
-                    const void *pg = sd.page[pages[j]].data;
-                    if (!apart(o, bp, sd.in[j].data, (size_t)2 * sd.pitch * c->N * sizeof(u64))) return CKKS_ERR_ARG;
-                    if (!same && !apart(o, bp, sd.out[pages[j]].data, bp)) return CKKS_ERR_ARG;
-                    if (!(same && o == pg) && !apart(o, bp, pg, bp)) return CKKS_ERR_ARG;
-                }
+        // descriptors: every side of the call on its own, then the buffers that are written against all others
+        struct Side { const ckks_ct *in, *page; ckks_ct *out; uint32_t level, pitch; };
+        std::vector<Side> sides;
+        if (in_k) sides.push_back(Side{in_k, page_k, out_k, 0, 0});
+        if (in_v) sides.push_back(Side{in_v, page_v, out_v, 0, 0});
+        uint32_t level = 0;
+        for (Side &sd : sides) {
+            for (uint32_t i = 0; i < n; i++) {
+                const ckks_ct &x = sd.in[i], &pg = sd.page[pages[i]];
+                if (!x.data || x.ncomp != 2 || !pg.data || pg.ncomp != 2 || !sd.out[pages[i]].data) return CKKS_ERR_ARG;
+            }
+            sd.pitch = sd.in[0].level; sd.level = sd.page[pages[0]].level;
+            if (!level) level = sd.level;
+            if (sd.level < 1 || sd.level != level || sd.pitch <= level || sd.pitch > c->L) return CKKS_ERR_LEVEL;
+            for (uint32_t i = 0; i < n; i++)
+                if (sd.in[i].level != sd.pitch || sd.page[pages[i]].level != level) return CKKS_ERR_LEVEL;
+            for (uint32_t i = 0; i < n; i++)
+                if (!scales_agree(sd.in[i].scale, sd.page[pages[i]].scale)) return CKKS_ERR_SCALE;
         }
-    for (uint32_t r = 0; r < p.nrot && rotated; r++)
-        if (!find_key(c, keys, nkeys, p.rots[r])) return CKKS_ERR_NO_KEY;
-    if (!ws || ws_bytes < ckks_cache_append_workspace_bytes(c, d, level, n)) return CKKS_ERR_WORKSPACE;
-    DeviceGuard guard(c->device);
-    std::vector<std::vector<Item>> items(sides.size());
-    for (size_t x = 0; x < sides.size(); x++)
-        for (uint32_t i = 0; i < n; i++)
-            items[x].push_back(Item{(const u64 *)sides[x].in[i].data, (const u64 *)sides[x].page[pages[i]].data, (u64 *)sides[x].out[pages[i]].data, spans[i].row, spans[i].begin,
-                                    spans[i].end});
-    // pages that are filled whole need no mask: with any of them the values go on their own
-    bool together = rotated && in_v;
-    for (uint32_t i = 0; i < n; i++) together = together && (spans[i].begin || spans[i].end < d->token_inner);
-    if (rotated)
-        rotate_items(c, d, p, items[0], sides[0].pitch, level + 1, cosv, sinv, keys, nkeys, ws, (cudaStream_t)stream, together ? &items[1] : nullptr, together ? sides[1].pitch : 0);
-    for (size_t x = rotated ? 1 : 0; x < sides.size() && !together; x++)
-        append_items(c, d->token_inner, items[x], sides[x].pitch, level + 1, ws, (cudaStream_t)stream);
-    rc = finish(c);
-    for (const Side &sd : sides)
-        for (uint32_t i = 0; i < n && rc == CKKS_OK; i++) {
-            sd.out[pages[i]].scale = sd.page[pages[i]].scale;
-            sd.out[pages[i]].level = level; sd.out[pages[i]].ncomp = 2;
-        }
-    return rc;
+        const size_t bp = (size_t)2 * level * c->N * sizeof(u64);
+        Buffers buffers;
+        for (const Side &sd : sides)
+            for (uint32_t i = 0; i < n; i++) {
+                const void *pg = sd.page[pages[i]].data, *o = sd.out[pages[i]].data;
+                buffers.read(sd.in[i].data, (size_t)2 * sd.pitch * c->N * sizeof(u64));
+                if (pg != o) buffers.read(pg, bp);
+                buffers.write(o, bp);
+            }
+        if (!buffers.apart()) return CKKS_ERR_ARG;
+        for (uint32_t r = 0; r < p.nrot && rotated; r++)
+            if (!find_key(c, keys, nkeys, p.rots[r])) return CKKS_ERR_NO_KEY;
+        if (!ws || ws_bytes < ckks_cache_append_workspace_bytes(c, d, level, n)) return CKKS_ERR_WORKSPACE;
+        DeviceGuard guard(c->device);
+        std::vector<std::vector<Item>> items(sides.size());
+        for (size_t x = 0; x < sides.size(); x++)
+            for (uint32_t i = 0; i < n; i++)
+                items[x].push_back(Item{(const u64 *)sides[x].in[i].data, (const u64 *)sides[x].page[pages[i]].data, (u64 *)sides[x].out[pages[i]].data, spans[i].row, spans[i].begin,
+                                        spans[i].end});
+        // pages that are filled whole need no mask: with any of them the values go on their own
+        bool together = rotated && in_v;
+        for (uint32_t i = 0; i < n; i++) together = together && (spans[i].begin || spans[i].end < d->token_inner);
+        if (rotated)
+            rotate_items(c, d, p, items[0], sides[0].pitch, level + 1, cosv, sinv, keys, nkeys, ws, (cudaStream_t)stream, together ? &items[1] : nullptr, together ? sides[1].pitch : 0);
+        for (size_t x = rotated ? 1 : 0; x < sides.size() && !together; x++)
+            append_items(c, d->token_inner, items[x], sides[x].pitch, level + 1, ws, (cudaStream_t)stream);
+        rc = finish(c);
+        for (const Side &sd : sides)
+            for (uint32_t i = 0; i < n && rc == CKKS_OK; i++) {
+                sd.out[pages[i]].scale = sd.page[pages[i]].scale;
+                sd.out[pages[i]].level = level; sd.out[pages[i]].ncomp = 2;
+            }
+        return rc;
+    });
 }

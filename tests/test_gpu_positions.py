@@ -420,6 +420,43 @@ def test_masks_and_differences_bit_exact(log_n, level, tokens, heads, E, Ti):
         assert np.array_equal(host(d[g].data), x[g]) and np.array_equal(host(e[g].data), y[g])
 
 
+def test_shapes_whose_products_leave_64_bits_are_refused():
+    _, ctx = _ring(10)
+    for tokens, heads, block in ((1 << 31, 4, 1 << 31), (1 << 31, 1 << 31, 4), (4, 1 << 31, 4), (1 << 30, 1, 1 << 30)):
+        _refused(binding.ERR_UNSUPPORTED, ctx.attention_rotations, tokens, heads, block)
+    for shape in ((1 << 31, 1 << 31, 4, 2), (4, 1 << 31, 1 << 31, 2), (1 << 16, 1 << 16, 1, 2), (512, 512, 512, 512)):
+        _refused(binding.ERR_UNSUPPORTED, ctx.rotary_rotations, *shape)
+
+
+def test_many_groups_and_a_ciphertext_in_several_places():
+    """512 groups of one score diagonal; one ciphertext as several inputs, and as both maps."""
+    import torch
+    from tests.gpu_util import host
+    P, ctx = _ring(10)
+    o, desc = P.oracle, AttnDesc(512, 1, 1)
+    x = _residues(P, 17, 2, 2)
+    d = _dev_cts(x)
+    out = ctx.attention_mask([d[g % 2] for g in range(512)], 512, 1, 1, causal=True, key_end=500)
+    for g in (0, 1, 15, 16, 255, 511):
+        want = o.rescale(o.mul_plain_acc(x[g % 2], o.encode(o.mask_slots(desc, g, True, 0, 500), float(P.q[1]), 2)))
+        assert np.array_equal(host(out[g].data), want), g
+    w = torch.tensor([1.0], dtype=torch.float64, device="cuda")
+    out = ctx.attention_difference([d[0]] * 2, [d[0]] * 2, w, 2, 1, 1)
+    want = o.attention_difference(AttnDesc(2, 1, 1), x[[0, 0]], x[[0, 0]], [1.0])
+    assert np.array_equal(host(out[0].data), want[0]) and np.array_equal(host(out[1].data), want[1])
+
+
+def test_weights_that_no_plaintext_holds_set_the_range_flag():
+    import torch
+    P, ctx = _ring(10)
+    x = _dev_cts(_residues(P, 1, 3, 2))
+    assert ctx.encode_range_flag() == binding.OK
+    for bad in (math.nan, math.inf, 1e6):
+        ctx.attention_difference(x, x, torch.tensor([0.5, bad], dtype=torch.float64, device="cuda"), 8, 2, 4)
+        assert ctx.encode_range_flag() == binding.ERR_RANGE
+        assert ctx.encode_range_flag() == binding.OK
+
+
 def test_masks_and_differences_of_unaligned_buffers():
     import torch
     from tests.gpu_util import host

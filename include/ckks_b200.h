@@ -138,11 +138,12 @@ const char *ckks_last_cuda_error(const ckks_ctx *ctx);
  *   CKKS_OPT_NTT_BULK_STORE 0 or 1 (default), kept for programs that set it: it chose between 128-byte bulk copies and 32-byte
  *                           accesses of the transforms' row passes, which now move 16 bytes per lane either way.
  *   CKKS_OPT_LANES          1..4 (default 4): streams over which ckks_attention_pack spreads its independent chains (one per
- *                           channel).  Lane 0 is the caller's stream, the others belong to the context; they are forked from and
+ *                           channel); ckks_rotary and ckks_cache_append of a few ciphertexts at log_n >= 15 use two of them.  Lane 0
+ *                           is the caller's stream, the others belong to the context; they are forked from and
  *                           joined to the caller's stream by events inside the call, so the call still behaves as work on the
- *                           caller's stream.  Its workspace size depends on it: set it before asking.  Results do not depend on it.
- *                           The lanes' streams and events belong to the context: two host threads must not run
- *                           ckks_attention_pack on the same context at the same time (use a context per thread).
+ *                           caller's stream.  ckks_attention_pack's workspace size depends on it: set it before asking.  Results do not
+ *                           depend on it.  The lanes' streams and events belong to the context: such calls of several host threads on one
+ *                           context enqueue one after the other, and none may be made while another of them is being captured into a graph.
  *   CKKS_OPT_STATIC_SCRATCH_BYTES  (read only) CKKS_STATIC_SCRATCH_BYTES of the loaded library.
  * set returns CKKS_ERR_ARG for an unknown option or a value outside its range; get returns -1 for an unknown option. */
 enum { CKKS_OPT_NTT_FP_SHARE = 1, CKKS_OPT_CONV_KERNEL = 2, CKKS_OPT_MAC_KERNEL = 3, CKKS_OPT_WAIT_CYCLES = 4,

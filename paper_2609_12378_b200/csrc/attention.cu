@@ -927,7 +927,7 @@ extern "C" int32_t ckks_attention_pack(ckks_ctx *c, const ckks_attn_desc *d, int
         }
     }
     // the channels are independent: spread over the lanes, each with its own buffers
-    const Lanes lanes(c, stream);
+    Lanes lanes(c, stream);
     lanes.fork();
     for (uint32_t dd = 0; dd < dim && !rc; dd++) {
         char *lb = base + L.lane + (dd % lanes.n) * L.lane_bytes;

@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include <exception>
+#include <mutex>
 #include <string>
 #include <vector>
 
@@ -86,36 +87,49 @@ struct ckks_ctx {
     int lanes = 4;
     cudaStream_t lane_stream[3] = {nullptr, nullptr, nullptr};
     cudaEvent_t lane_event[4] = {nullptr, nullptr, nullptr, nullptr};
+    std::mutex lane_mutex;
 };
 
 // The context's streams as lanes for independent chains: lane 0 is the caller's stream.  fork() makes the other lanes wait
-// for what the caller's stream has been given so far, join() makes the caller's stream wait for all of them.
+// for what the caller's stream has been given so far, join() makes the caller's stream wait for all of them.  One call at a time enqueues
+// between the two (other threads' calls on the context wait here), because the events are the context's.
 struct Lanes {
     ckks_ctx *c;
     cudaStream_t caller;
     uint32_t n;
-    Lanes(ckks_ctx *ctx, void *stream) : c(ctx), caller((cudaStream_t)stream), n((uint32_t)std::max(1, std::min(ctx->lanes, 4))) {}
+    std::unique_lock<std::mutex> lock;
+    uint32_t forked = 0;          // lanes besides the caller's that have to be joined
+    Lanes(ckks_ctx *ctx, void *stream, bool use = true) : c(ctx), caller((cudaStream_t)stream), n(use ? (uint32_t)std::max(1, std::min(ctx->lanes, 4)) : 1) {
+        if (n > 1) lock = std::unique_lock<std::mutex>(c->lane_mutex);
+    }
+    ~Lanes() { join(); }
     void *at(uint32_t i) const { return i % n == 0 ? (void *)caller : (void *)c->lane_stream[i % n - 1]; }
-    void fork() const {
+    // used: lanes besides the caller's (all of them unless given)
+    void fork(uint32_t used = 3) {
         if (n == 1) return;
         int prev = 0;
         cudaGetDevice(&prev);
         cudaSetDevice(c->device);
+        forked = std::min(used, n - 1);
         cudaEventRecord(c->lane_event[0], caller);
-        for (uint32_t i = 1; i < n; i++) cudaStreamWaitEvent(c->lane_stream[i - 1], c->lane_event[0], 0);
+        for (uint32_t i = 1; i <= forked; i++) cudaStreamWaitEvent(c->lane_stream[i - 1], c->lane_event[0], 0);
         cudaSetDevice(prev);
     }
-    void join() const {
-        if (n == 1) return;
+    void join() {
+        if (!forked) return;
         int prev = 0;
         cudaGetDevice(&prev);
         cudaSetDevice(c->device);
-        for (uint32_t i = 1; i < n; i++) {
+        for (uint32_t i = 1; i <= forked; i++) {
             cudaEventRecord(c->lane_event[i], c->lane_stream[i - 1]);
             cudaStreamWaitEvent(caller, c->lane_event[i], 0);
         }
+        forked = 0;
         cudaSetDevice(prev);
     }
+    // what lane i has been given so far, and the caller's stream waiting for it (on the context's device)
+    void mark(uint32_t i) const { cudaEventRecord(c->lane_event[i], c->lane_stream[i - 1]); }
+    void wait(uint32_t i) const { cudaStreamWaitEvent(caller, c->lane_event[i], 0); }
 };
 inline uint32_t lane_count(const ckks_ctx *c) { return (uint32_t)std::max(1, std::min(c->lanes, 4)); }
 

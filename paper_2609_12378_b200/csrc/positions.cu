@@ -137,12 +137,29 @@ const ckks_evk *find_key(const ckks_ctx *c, const ckks_evk *keys, uint32_t nkeys
     return nullptr;
 }
 
+// Calls of a few ciphertexts on large rings, whose launches leave most of the GPU idle, run what does not depend on each other side by side: the
+// plaintexts' encoding next to the extension of the digits, the values next to the keys (one token's append at N = 2^16, level 18, 213 -> 180 us).
+// Smaller rings' short calls are bound by the host, to which the fork's events cost more than it gains.
+bool side_by_side(const ckks_ctx *c, uint32_t n) { return c->log_n >= 15 && n <= (4u << (16 - c->log_n)); }
+
 // Workspace of a pass over up to `m` sets of positions and `m` ciphertexts side by side: plaintexts, then the encoder's scratch, whose
-// place the key switches take over
-size_t rotary_bytes(const ckks_ctx *c, uint32_t level, uint32_t nrot, bool mask, uint32_t m) {
-    const size_t N = c->N * sizeof(u64), pts = (size_t)m * (1 + nrot + mask) * (level + c->K) * N;
-    return align256(pts) + align256(std::max(encode_workspace_bytes(c, m * (1 + nrot + mask)), (size_t)m * ks_workspace_limbs(c, level) * N));
+// place the key switches take over (side by side: behind it), and after them the values'
+struct RotaryWs { size_t rest, ks, values, bytes; };
+RotaryWs rotary_ws(const ckks_ctx *c, uint32_t level, uint32_t nrot, bool mask, uint32_t m) {
+    const size_t N = c->N * sizeof(u64), enc = align256(encode_workspace_bytes(c, m * (1 + nrot + mask))), ks = align256((size_t)m * ks_workspace_limbs(c, level) * N);
+    RotaryWs w;
+    w.rest = align256((size_t)m * (1 + nrot + mask) * (level + c->K) * N);
+    if (!side_by_side(c, m)) {
+        w.ks = w.values = w.rest;
+        w.bytes = w.rest + std::max(enc, ks);
+        return w;
+    }
+    w.ks = w.rest + enc;
+    w.values = w.ks + ks;
+    w.bytes = w.values + (mask ? align256(plain_rescale_limbs(level, m) * N) : 0);
+    return w;
 }
+size_t rotary_bytes(const ckks_ctx *c, uint32_t level, uint32_t nrot, bool mask, uint32_t m) { return rotary_ws(c, level, nrot, mask, m).bytes; }
 size_t mask_bytes(const ckks_ctx *c, uint32_t level, uint32_t m) {
     const size_t N = c->N * sizeof(u64);
     return align256((size_t)m * level * N) + align256(std::max(encode_workspace_bytes(c, m), plain_rescale_limbs(level, m) * N));
@@ -171,8 +188,14 @@ void rotate_items(ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, c
     const uint32_t nt = level + c->K, beta = (level + c->alpha - 1) / c->alpha, m = std::min((uint32_t)items.size(), KS_MULTI);
     const double scale = (double)c->mod[level - 1];
     const uint32_t kinds = 1 + p.nrot + (values ? 1 : 0);        // a set: C, the S_r, the mask, each level + K limbs apart
+    const RotaryWs at = rotary_ws(c, level, p.nrot, values != nullptr, m);
     u64 *pts = (u64 *)ws;
-    void *rest = (char *)ws + align256((size_t)m * kinds * nt * N * sizeof(u64));
+    void *rest = (char *)ws + at.rest, *ksw = (char *)ws + at.ks, *vws = (char *)ws + at.values;
+    // lane 1 (the caller's stream where the call does not fork): plaintexts, then the values
+    Lanes lanes(c, s, side_by_side(c, (uint32_t)items.size()));
+    const bool fork = lanes.n > 1;
+    cudaStream_t side = fork ? (cudaStream_t)lanes.at(1) : s;
+    if (fork) lanes.fork(1);
     for (uint32_t s0 = 0; s0 < sets.size(); s0 += SLOT_SETS) {
         const uint32_t ns = std::min(SLOT_SETS, (uint32_t)sets.size() - s0);
         SlotPositions slots{cosv, sinv, d->dim, d->heads, d->token_inner, d->rot_dim, d->layout == CKKS_ROTARY_INTERLEAVED, d->row_step, p.nrot, kinds, {}, {}, {}};
@@ -183,11 +206,12 @@ void rotate_items(ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, c
             for (uint32_t i : sets[s0 + k]) todo.emplace_back(i, k);
         }
         const uint32_t batch = ns * kinds;
-        launch_encode_slots(c, slots, batch, scale, rest, s);
-        launch_encode_coefs(c, rest, batch, 0, batch * nt, set_map(level, p.nrot, kinds, c->K, c->L), pts, s, true);
+        launch_encode_slots(c, slots, batch, scale, rest, side);
+        launch_encode_coefs(c, rest, batch, 0, batch * nt, set_map(level, p.nrot, kinds, c->K, c->L), pts, side, true);
+        if (fork) lanes.mark(1);
         for (size_t i0 = 0; i0 < todo.size(); i0 += KS_MULTI) {
             const uint32_t nb = (uint32_t)std::min<size_t>(KS_MULTI, todo.size() - i0);
-            KsWorkspace w = ks_carve(c, level, rest, nb);
+            KsWorkspace w = ks_carve(c, level, ksw, nb);
             w.alone = items.size() == 1;
             PosArgs a{};
             Ptrs c1, out, acc;
@@ -203,25 +227,30 @@ void rotate_items(ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, c
                 a.evk[r] = (const u64 *)k->data; a.galois[r] = k->galois;
             }
             w.mid = ks_mid(c, level, w, c1, a.evk, p.nrot) && aligned16(a.c) && aligned16(pts);
+            auto append_values = [&]() {
+                PlainRescale v{};
+                v.in.n = v.pt.n = v.acc.n = v.out.n = nb;
+                v.pitch = values_pitch; v.acc_pitch = level - 1; v.level = level; v.add = true;
+                for (uint32_t b = 0; b < nb; b++) {
+                    const Item &it = (*values)[todo[i0 + b].first];
+                    v.in.p[b] = it.in; v.acc.p[b] = it.acc; v.out.p[b] = it.out;
+                    v.pt.p[b] = pts + (todo[i0 + b].second * (size_t)kinds + kinds - 1) * nt * N;
+                }
+                launch_plain_rescale(c, v, (u64 *)vws, side, nb);
+            };
+            if (values && !fork) append_values();        // its scratch is the key switches'
             ks_modup(c, c1, level, w, s, nb);
+            if (values && fork) append_values();
             a.ext = w.ext; a.u = w.u; a.own = pts; a.fac = pts + (size_t)nt * N;
             a.own_set = a.fac_set = (size_t)kinds * nt * N; a.fac_rot = (size_t)nt * N;
             a.pitch = pitch; a.nrot = p.nrot; a.nb = nb; a.level = level; a.inv_from = level - 1;
+            if (fork) lanes.wait(1);
             if (w.mid) launch_mid_rows_pos(c, a, beta, s);
             else launch(positions_inner, dim3(c->N / THREADS, nb, nt), THREADS, 0, s, c->dev, a);
             ks_down_rescale(c, level, w, out, items[0].acc ? &acc : nullptr, s, nb);
-            if (!values) continue;
-            PlainRescale v{};
-            v.in.n = v.pt.n = v.acc.n = v.out.n = nb;
-            v.pitch = values_pitch; v.acc_pitch = level - 1; v.level = level; v.add = true;
-            for (uint32_t b = 0; b < nb; b++) {
-                const Item &it = (*values)[todo[i0 + b].first];
-                v.in.p[b] = it.in; v.acc.p[b] = it.acc; v.out.p[b] = it.out;
-                v.pt.p[b] = pts + (todo[i0 + b].second * (size_t)kinds + kinds - 1) * nt * N;
-            }
-            launch_plain_rescale(c, v, (u64 *)rest, s, nb);
         }
     }
+    lanes.join();
 }
 
 // Values (or keys without positions): tokens that fill their page are added as they are, others under a mask

@@ -3,6 +3,7 @@ maps, and masked and differential attention.  Every limb bit-exact against the C
 decrypted results."""
 import ctypes as C
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -15,7 +16,7 @@ from tests.test_oracle_positions import TOL, rotate_clear
 pytestmark = pytest.mark.gpu
 
 SCALE = 2.0 ** 50
-RINGS = {10: (10, 6, 3, 2), 11: (11, 6, 1, 6), 12: (12, 6, 2, 3), 13: (13, 7, 7, 1)}       # log_n: parameters, by ring of the cases
+RINGS = {10: (10, 6, 3, 2), 11: (11, 6, 1, 6), 12: (12, 6, 2, 3), 13: (13, 7, 7, 1), 15: (15, 4, 2, 2), 16: (16, 3, 1, 3)}       # log_n: parameters, by ring of the cases
 
 
 def _ring(log_n):
@@ -136,6 +137,9 @@ CASES = [
     (12, 3, 64, 32, 1, 64, "half", 19, list(range(19)), False),         # more ciphertexts than run side by side, one token each
     (12, 4, 32, 4, 16, 32, "half", 20, [16 * (i % 17) for i in range(20)], False),   # more sets of positions than are encoded at a time
     (13, 7, 64, 8, 8, 2, "half", 1, [0], False),                        # one digit; one pair rotated
+    (15, 4, 64, 16, 16, 64, "half", 2, [0, 16], False),                 # side by side: the plaintexts' encoding next to the digits
+    (15, 3, 64, 16, 8, 40, "interleaved", 9, [i % 4 for i in range(9)], True),       # one more than run side by side
+    (16, 3, 128, 32, 8, 128, "half", 1, [3], True),
 ]
 
 
@@ -213,16 +217,17 @@ def test_rotation_with_other_options_and_on_another_stream():
     assert all(np.array_equal(host(out[i].data), want[i]) for i in range(3))
 
 
-def test_rotation_and_append_replay_from_a_graph():
-    """Captured once, replayed on new inputs, tables and pages in the same buffers."""
+@pytest.mark.parametrize("log_n,top", [(12, 5), (15, 4)])
+def test_rotation_and_append_replay_from_a_graph(log_n, top):
+    """Captured once, replayed on new inputs, tables and pages in the same buffers, an eager call between the replays."""
     import torch
     from tests.gpu_util import host
-    P, ctx = _ring(12)
+    P, ctx = _ring(log_n)
     o, a = P.oracle, (32, 4, 16)
     rots = o.rotary_rotations(*a, 32, False)
     keys = _keys(P, 24, rots)
     dk = _dev_keys(keys)
-    x, v, pk = (_residues(P, s, l, 1) for s, l in ((1, 5), (2, 5), (3, 4)))
+    x, v, pk = (_residues(P, s, l, 1) for s, l in ((1, top), (2, top), (3, top - 1)))
     d, dv, dp = _dev_cts(x), _dev_cts(v), _dev_cts(pk)
     cos, sin, dc, ds = _table(3, 16, 16)
     outs = [[binding.Ciphertext(torch.empty_like(dp[0].data), 0.0)] for _ in range(3)]
@@ -231,7 +236,7 @@ def test_rotation_and_append_replay_from_a_graph():
         ctx.rotary(d, [0], dc, ds, dk, *a, outs=outs[0], ws=ws)
         ctx.cache_append(d, dv, [0], [(3, 9, 0)], dp, dp, dc, ds, dk, *a, out_k=outs[1], out_v=outs[2], ws=ws)
     L, desc = binding.load(), ctx._rotary_desc(*a, None, "half")
-    ws = torch.empty(max(L.ckks_rotary_workspace_bytes(ctx._h, C.byref(desc), 5, 1), L.ckks_cache_append_workspace_bytes(ctx._h, C.byref(desc), 4, 1)),
+    ws = torch.empty(max(L.ckks_rotary_workspace_bytes(ctx._h, C.byref(desc), top, 1), L.ckks_cache_append_workspace_bytes(ctx._h, C.byref(desc), top - 1, 1)),
                      dtype=torch.uint8, device="cuda")
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
@@ -241,15 +246,53 @@ def test_rotation_and_append_replay_from_a_graph():
     with torch.cuda.graph(graph):
         step()
     for seed in (31, 32):
-        x, v, pk = (_residues(P, seed + s, l, 1) for s, l in ((1, 5), (2, 5), (3, 4)))
+        x, v, pk = (_residues(P, seed + s, l, 1) for s, l in ((1, top), (2, top), (3, top - 1)))
         c2, s2, _, _ = _table(seed, 16, 16)
         for t, arr in ((d[0].data, x[0]), (dv[0].data, v[0]), (dp[0].data, pk[0])):
             t.view(torch.int64).copy_(torch.from_numpy(arr.view(np.int64)))
         dc.copy_(torch.from_numpy(c2)); ds.copy_(torch.from_numpy(s2))
         graph.replay()
-        assert np.array_equal(host(outs[0][0].data), o.rotary(x, [0], c2, s2, keys, *a, 32, False)[0])
+        eager = ctx.rotary(d, [0], dc, ds, dk, *a)[0]
+        want = o.rotary(x, [0], c2, s2, keys, *a, 32, False)[0]
+        assert np.array_equal(host(outs[0][0].data), want) and np.array_equal(host(eager.data), want)
         assert np.array_equal(host(outs[1][0].data), o.append_keys(pk[0], x[0], c2, s2, keys, *a, 32, False, 3, 9, 0))
         assert np.array_equal(host(outs[2][0].data), o.append_values(pk[0], v[0], 16, 3, 9))
+
+
+def test_calls_on_two_streams_of_one_context():
+    """Each with a workspace of its own, nothing ordering one after the other, from one host thread and from two; with one lane and with several."""
+    import torch
+    from tests.gpu_util import host
+    P, ctx = _ring(15)
+    o, a = P.oracle, (64, 16, 16)
+    keys = _keys(P, 33, o.rotary_rotations(*a, 64, False))
+    x, v, pk = _residues(P, 34, 4, 2), _residues(P, 35, 4, 2), _residues(P, 36, 3, 2)
+    cos, sin, dc, ds = _table(37, 16, 32)
+    d, dv, dp, dk = _dev_cts(x), _dev_cts(v), _dev_cts(pk), _dev_keys(keys)
+    want_k = [o.append_keys(pk[i], x[i], cos, sin, keys, *a, 64, False, 2, 7, 1) for i in range(2)]
+    want_v = [o.append_values(pk[i], v[i], 16, 2, 7) for i in range(2)]
+    need = int(binding.load().ckks_cache_append_workspace_bytes(ctx._h, C.byref(ctx._rotary_desc(*a, None, "half")), 3, 1))
+    for lanes in (1, 2, 4):
+        old = ctx.get_option(binding.OPT_LANES)
+        ctx.set_option(binding.OPT_LANES, lanes)
+        try:
+            streams = [torch.cuda.Stream() for _ in range(2)]
+            wss = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(2)]
+            outs = [[_dev_cts(np.zeros_like(pk[:1])) for _ in range(2)] for _ in range(2)]
+            torch.cuda.synchronize()
+
+            def call(i):
+                ctx.cache_append([d[i]], [dv[i]], [0], [(2, 7, 1)], [dp[i]], [dp[i]], dc, ds, dk, *a, out_k=outs[i][0], out_v=outs[i][1], ws=wss[i], stream=streams[i])
+            for _ in range(3):
+                call(0), call(1)
+            # and from two host threads
+            threads = [threading.Thread(target=lambda i=i: [call(i) for _ in range(20)]) for i in range(2)]
+            [t.start() for t in threads], [t.join() for t in threads]
+            torch.cuda.synchronize()
+        finally:
+            ctx.set_option(binding.OPT_LANES, old)
+        for i in range(2):
+            assert np.array_equal(host(outs[i][0][0].data), want_k[i]) and np.array_equal(host(outs[i][1][0].data), want_v[i]), (lanes, i)
 
 
 def _refused(code, f, *args, **kw):
@@ -308,6 +351,8 @@ APPENDS = [
     (10, 3, 6, 16, 2, 8, 12, "half", 5, [4, 1, 2], [(0, 8, 0), (0, 8, 8), (0, 3, 16)]),                  # a prompt; inputs of a higher level
     (10, 1, 2, 16, 4, 8, 16, "interleaved", 3, [2, 0], [(7, 8, 0), (1, 7, 5)]),                          # the lowest page level; copies of rows
     (11, 5, 6, 32, 8, 4, 32, "half", 2, [1], [(0, 1, 3)]),                                               # six digits
+    (15, 3, 4, 64, 16, 16, 64, "half", 3, [1, 2], [(0, 1, 0), (3, 16, 5)]),                                 # keys and values side by side
+    (15, 2, 4, 64, 16, 16, 30, "interleaved", 2, [1, 0], [(0, 16, 0), (2, 9, 0)]),                       # a whole page among them
     (12, 5, 6, 32, 4, 16, 20, "interleaved", 20, [19 - i for i in range(18)], [(i % 5, 16 - i % 3, i) for i in range(18)]),
 ]
 

@@ -225,7 +225,7 @@ static void mask_groups(const ckks_ctx *c, const AttnPlan &p, const ckks_attn_ma
     void *rest = (char *)ws + align256(std::min(p.G, KS_MULTI) * ptw * sizeof(u64));
     for (uint32_t g0 = 0; g0 < p.G; g0 += KS_MULTI) {
         const uint32_t nb = std::min(KS_MULTI, p.G - g0);
-        const SlotScores slots{p.Tk, p.H, p.E, p.Ti, p.R, g0, m.causal, m.key_begin, m.key_end, m.window, (long long)m.query_offset};
+        const SlotScores slots{log2_of(p.Tk), log2_of(p.H), log2_of(p.Ti), log2_of(p.R), p.E, g0, m.causal, m.key_begin, m.key_end, m.window, (long long)m.query_offset};
         PlainRescale a{};
         a.in.n = a.out.n = nb;
         for (uint32_t b = 0; b < nb; b++) { a.in.p[b] = in[g0 + b]; a.out.p[b] = out[g0 + b]; }
@@ -241,7 +241,7 @@ static void difference_groups(const ckks_ctx *c, const AttnPlan &p, const double
                               cudaStream_t s) {
     u64 *pt = (u64 *)ws;
     void *rest = (char *)ws + align256((size_t)level * c->N * sizeof(u64));
-    launch_encode_slots(c, SlotHeads{weights, p.H, p.Ti, p.R}, 1, (double)c->mod[level - 1], rest, s);
+    launch_encode_slots(c, SlotHeads{weights, log2_of(p.H), log2_of(p.Ti), log2_of(p.R)}, 1, (double)c->mod[level - 1], rest, s);
     launch_encode_coefs(c, rest, 1, 0, level, plain_map(0, level), pt, s);
     for (uint32_t g0 = 0; g0 < p.G; g0 += KS_MULTI) {
         const uint32_t nb = std::min(KS_MULTI, p.G - g0);

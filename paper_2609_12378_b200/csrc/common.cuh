@@ -644,19 +644,21 @@ constexpr uint32_t SLOT_SETS = KS_MULTI;
 // [..][rot / 2], the others zeros.
 struct SlotPositions {
     const double *cos, *sin;
-    uint32_t dim, heads, inner, rot, interleaved, step, nrot, kinds;
+    uint32_t dim, heads, inner, rot, interleaved, step, nrot, kinds;       // dim, heads, inner: their logarithms (they divide the slots)
     uint32_t row[SLOT_SETS], begin[SLOT_SETS], end[SLOT_SETS];
 };
 // 1.0 for the tokens begin <= t < end of a shard ciphertext
-struct SlotTokens { uint32_t inner, begin[SLOT_SETS], end[SLOT_SETS]; };
+struct SlotTokens { uint32_t inner /* logarithm */, begin[SLOT_SETS], end[SLOT_SETS]; };
 // Score ciphertexts, slot ((((e P + pos) heads + h) inner + t) copies + r): 1.0 where query i sees the key token of group g0 + b
 struct SlotScores {
-    uint32_t tokens, heads, block, inner, copies, g0;
+    uint32_t tokens, heads, inner, copies;          // logarithms
+    uint32_t block, g0;
     uint32_t causal, key_begin, key_end, window;
     long long offset;
 };
 // -weights[h] (device)
-struct SlotHeads { const double *weights; uint32_t heads, inner, copies; };
+struct SlotHeads { const double *weights; uint32_t heads, inner, copies /* logarithms */; };
+inline uint32_t log2_of(uint32_t pow2) { return (uint32_t)__builtin_ctz(pow2); }
 // The coefficients of `batch` <= 65535 plaintexts, formed in ws (encode_workspace_bytes), and the transform of the ones from `first` on to the limbs
 // of map (count limbs in all)
 template <class Slots>

@@ -32,12 +32,12 @@ __device__ __forceinline__ double2 slot_value(const SlotArray &a, uint32_t b, ui
     return make_double2(a.re[(size_t)b * n + j], a.im ? a.im[(size_t)b * n + j] : 0.0);
 }
 __device__ __forceinline__ double2 slot_value(const SlotPositions &a, uint32_t b, uint32_t j, uint32_t) {
-    const uint32_t kind = b % a.kinds, set = b / a.kinds, t = j % a.inner, d = j / (a.inner * a.heads) % a.dim, half = a.rot / 2;
+    const uint32_t kind = b % a.kinds, set = b / a.kinds, t = j & ((1u << a.inner) - 1), d = j >> (a.inner + a.heads) & ((1u << a.dim) - 1), half = a.rot >> 1;
     if (t < a.begin[set] || t >= a.end[set]) return make_double2(0.0, 0.0);
     if (kind > a.nrot) return make_double2(1.0, 0.0);
     if (d >= a.rot) return make_double2(kind ? 0.0 : 1.0, 0.0);
-    const uint32_t pair = a.interleaved ? d >> 1 : d % half;
     const bool second = a.interleaved ? d & 1 : d >= half;
+    const uint32_t pair = a.interleaved ? d >> 1 : second ? d - half : d;
     const size_t at = ((size_t)a.row[set] + (size_t)(t - a.begin[set]) * a.step) * half + pair;
     if (!kind) return make_double2(a.cos[at], 0.0);
     // one rotation serves both channels of a pair; of two, the first (to the left) serves the first channel, the other the second
@@ -45,22 +45,22 @@ __device__ __forceinline__ double2 slot_value(const SlotPositions &a, uint32_t b
     return make_double2(second ? a.sin[at] : -a.sin[at], 0.0);
 }
 __device__ __forceinline__ double2 slot_value(const SlotTokens &a, uint32_t b, uint32_t j, uint32_t) {
-    const uint32_t t = j % a.inner;
+    const uint32_t t = j & ((1u << a.inner) - 1);
     return make_double2(t >= a.begin[b] && t < a.end[b] ? 1.0 : 0.0, 0.0);
 }
 __device__ __forceinline__ double2 slot_value(const SlotScores &a, uint32_t b, uint32_t j, uint32_t) {
-    const uint32_t x = j / a.copies, pos = x / (a.inner * a.heads), per = a.tokens / a.inner;
-    const uint32_t e = pos / per, i = pos % per * a.inner + x % a.inner;
+    const uint32_t x = j >> a.copies, pos = x >> (a.inner + a.heads), per = a.tokens - a.inner, tokens = 1u << a.tokens;
+    const uint32_t e = pos >> per, i = ((pos & ((1u << per) - 1)) << a.inner) + (x & ((1u << a.inner) - 1));
     // the key operand holds token (i + e) mod tokens in block e; group g is its rotation by g blocks' tokens over (e, i)
     uint32_t f = i + (a.g0 + b) * a.block, fe = e;
-    if (f >= a.tokens) { f -= a.tokens; fe = e + 1 == a.block ? 0 : e + 1; }
-    const uint32_t key = (f + fe) % a.tokens;
+    if (f >= tokens) { f -= tokens; fe = e + 1 == a.block ? 0 : e + 1; }
+    const uint32_t key = (f + fe) & (tokens - 1);
     const long long at = (long long)i + a.offset;
     const bool live = key >= a.key_begin && key < a.key_end && (!a.causal || (long long)key <= at) && (!a.window || (long long)key > at - (long long)a.window);
     return make_double2(live ? 1.0 : 0.0, 0.0);
 }
 __device__ __forceinline__ double2 slot_value(const SlotHeads &a, uint32_t, uint32_t j, uint32_t) {
-    return make_double2(-a.weights[j / (a.copies * a.inner) % a.heads], 0.0);
+    return make_double2(-a.weights[j >> (a.copies + a.inner) & ((1u << a.heads) - 1)], 0.0);
 }
 
 // Pass 1: gather (E1 + bit reversal), stages m = 2 .. min(n, CH) on chunks of CH points.  The stages' twiddles come from

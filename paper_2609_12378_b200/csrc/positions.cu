@@ -198,7 +198,7 @@ void rotate_items(ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, c
     if (fork) lanes.fork(1);
     for (uint32_t s0 = 0; s0 < sets.size(); s0 += SLOT_SETS) {
         const uint32_t ns = std::min(SLOT_SETS, (uint32_t)sets.size() - s0);
-        SlotPositions slots{cosv, sinv, d->dim, d->heads, d->token_inner, d->rot_dim, d->layout == CKKS_ROTARY_INTERLEAVED, d->row_step, p.nrot, kinds, {}, {}, {}};
+        SlotPositions slots{cosv, sinv, log2_of(d->dim), log2_of(d->heads), log2_of(d->token_inner), d->rot_dim, d->layout == CKKS_ROTARY_INTERLEAVED, d->row_step, p.nrot, kinds, {}, {}, {}};
         std::vector<std::pair<uint32_t, uint32_t>> todo;               // (item, set)
         for (uint32_t k = 0; k < ns; k++) {
             const Item &it = items[sets[s0 + k][0]];
@@ -270,7 +270,7 @@ void append_items(ckks_ctx *c, uint32_t token_inner, const std::vector<Item> &it
     }
     for (size_t i0 = 0; i0 < part.size(); i0 += KS_MULTI) {
         const uint32_t nb = (uint32_t)std::min<size_t>(KS_MULTI, part.size() - i0);
-        SlotTokens slots{token_inner, {}, {}};
+        SlotTokens slots{log2_of(token_inner), {}, {}};
         PlainRescale pr{};
         pr.in.n = pr.acc.n = pr.out.n = nb;
         pr.pt = Ptrs(pts, level * N);

@@ -768,13 +768,17 @@ class Context:
         f = CRotaryScaling(ROTARY_SCALINGS[scaling], rot_dim, theta, factor, original_length, turns_few, turns_many, magnitude)
         shape = (count, rot_dim // 2)
         if out is None:
-            out = tuple(torch.empty(shape, dtype=torch.float64, device=self.device) for _ in range(2))
+            out = (torch.empty(shape, dtype=torch.float64, device=self.device), torch.empty(shape, dtype=torch.float64, device=self.device))
+        else:
+            self._table_out(out, shape)
+        self._check(_lib.ckks_rotary_table(self._h, C.byref(f), first, count, out[0].data_ptr(), out[1].data_ptr(), _stream_ptr(stream)))
+        return out
+
+    def _table_out(self, out, shape):
         for t in out:
             if not (t.is_cuda and t.dtype == torch.float64 and t.is_contiguous() and tuple(t.shape) == shape):
                 raise TypeError("expected contiguous CUDA float64 tensors [count][rot_dim / 2]")
             self._here(t)
-        self._check(_lib.ckks_rotary_table(self._h, C.byref(f), first, count, out[0].data_ptr(), out[1].data_ptr(), _stream_ptr(stream)))
-        return out
 
     @staticmethod
     def _rotary_shape(dim, heads, token_inner, rot_dim, layout, same_position=False):

@@ -126,7 +126,12 @@ __global__ void __launch_bounds__(32 * MID_ROWS, TERMS ? 5 : 8) mid_rows(DevTabl
 }
 
 // The same for rotations whose results are multiplied by plaintexts (PosArgs): every rotation reads the one set of digits through its own
-// permutation, its sums meet their factor S_r in registers, and the ciphertext's own term comes on top.
+// permutation, its sums meet their factor S_r in registers, and the ciphertext's own term comes on top.  Products are summed exactly and reduced
+// once (ProductSum).  Bound by two pipes at a time, FP64 65 % and the load/store unit's shared-memory and L1 passes 69 % of their cycles (sixteen
+// ciphertexts at N = 2^16, level 24: 563 us; 656 with every product reduced and the sums of a row kept until its end).  Warps of a CTA take the
+// same row of up to four ciphertexts, which share its key words, twiddles and often plaintexts in L1 (L2 hits instead: 3 % more).  Tried and
+// slower or no faster there: the words on their way to L2 ahead of the digits' transforms (629 us then, no change), the row's twiddles in
+// shared memory (no change), one component after the other (632), eight CTAs per SM at 64 registers (578, spilling).
 struct PosRow {            // a warp's place
     uint32_t t, rl, row, R, bz, nt, x, kt, own, set;
     double q, qinv, pq;
@@ -220,7 +225,8 @@ __device__ __forceinline__ void pos_inverse(const DevTables &c, const PosRow &p,
     __syncwarp();
 }
 
-// One rotation: pair by pair, nothing is held from one to the next; the pairs of a limb that is transformed back wait in their place in u
+// One rotation: pair by pair, nothing is held from one to the next; the pairs of a limb that is transformed back wait in their place in u.  One
+// ciphertext at level 18: 41 us.
 template <uint32_t BETA>
 __global__ void __launch_bounds__(32 * MID_ROWS, 6) mid_rows_pos(DevTables c, const __grid_constant__ PosArgs a) {
     __shared__ __align__(16) double sm[BETA][MID_ROWS][WROW_PAD];
@@ -259,7 +265,8 @@ __global__ void __launch_bounds__(32 * MID_ROWS, 6) mid_rows_pos(DevTables c, co
     }
 }
 
-// Several rotations: their sums stay in registers, five CTAs per SM
+// Several rotations: their sums stay in registers, five CTAs per SM (two rotations of six ciphertexts at N = 2^15, level 10: 103 us; with ciphertexts
+// sharing a CTA 131: six do not fill the groups of four)
 template <uint32_t BETA>
 __global__ void __launch_bounds__(32 * MID_ROWS, 5) mid_rows_pos_sum(DevTables c, const __grid_constant__ PosArgs a) {
     __shared__ __align__(16) double sm[BETA][MID_ROWS][WROW_PAD];

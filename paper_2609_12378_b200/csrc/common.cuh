@@ -293,6 +293,12 @@ struct ProductSum {
         const double k = __dsub_rn(__fma_rn(__dadd_rn(hs, l), qinv, MAGIC1), MAGIC1);
         return __dadd_rn(__fma_rn(-k, q, hs), l);
     }
+    // room for further products: the sum reduced to half a prime
+    __device__ __forceinline__ void carry(double q, double qinv) {
+        const double s = sum(q, qinv), k = __dsub_rn(__fma_rn(s, qinv, MAGIC0), MAGIC0);
+        l = __fma_rn(-k, q, s);
+        h = SUM_SIGMA;
+    }
 };
 __device__ __forceinline__ double u64_to_d(u64 x) { return __dsub_rn(__longlong_as_double((long long)(x | 0x4330000000000000ull)), TWO52); }
 __device__ __forceinline__ u64 d_to_u64(double v) { return (u64)__double_as_longlong(__dadd_rn(v, TWO52)) & 0x000FFFFFFFFFFFFFull; }
@@ -533,7 +539,7 @@ struct KsOut {
 };
 void ks_moddown(const ckks_ctx *c, uint32_t level, const KsWorkspace &w, const KsOut &o, cudaStream_t s, uint32_t nb = 1, const KsMulti *multi = nullptr);
 // Whether launch_mid_rows takes the digits d of key switches, which serve one key each (nkeys keys in all)
-bool ks_mid(const ckks_ctx *c, uint32_t level, const KsWorkspace &w, const Ptrs &d, const u64 *const *evk, uint32_t nkeys);
+bool ks_mid(const ckks_ctx *c, uint32_t level, const KsWorkspace &w, const Ptrs &d, const u64 *const *evk, uint32_t nkeys, uint32_t max_beta = IP_FUSED_BETA);
 // and whether it is to take a sum of nterm terms of nb entries each
 bool ks_mid_sum(const ckks_ctx *c, uint32_t level, uint32_t nterm, uint32_t nb);
 // Both together: out = ModDown(<digits, key>) and the final combination, digits read through the permutation of o.galois
@@ -577,7 +583,7 @@ void launch_mid_rows(const ckks_ctx *c, const MidArgs &a, uint32_t beta, cudaStr
 //   u[b][k] = sum_{r < nrot} S_r ( <ext[b] read through sigma_r, evk_r>_k + [k = 0] P sigma_r(c0) ) + P C c_k,   c = c[b],
 // S_r of set s at fac + r fac_rot + s fac_set ([level + K][N]), C at own + s own_set ([level][N]), s = set[b]; the terms with P on the
 // q-limbs alone.  Component 1 of c[b] lies `pitch` limbs behind component 0; digits that have a limb among their own read it there.
-constexpr uint32_t POS_ROT = 2;
+constexpr uint32_t POS_ROT = 2, POS_BETA = 8;       // rotations, digits that launch_mid_rows_pos takes
 struct PosArgs {
     const u64 *ext, *evk[POS_ROT], *own, *fac;
     u64 galois[POS_ROT];

@@ -137,11 +137,10 @@ struct PosRow {            // a warp's place
     double q, qinv, pq;
     size_t limb, cc, kc;
 };
-__device__ __forceinline__ PosRow pos_row(const DevTables &c, const PosArgs &a, uint32_t beta) {
+__device__ __forceinline__ PosRow pos_row(const DevTables &c, const PosArgs &a, uint32_t beta, uint32_t row, uint32_t bz) {
     PosRow p;
     p.t = threadIdx.x & 31; p.rl = threadIdx.x >> 5; p.R = c.N >> 8;
-    p.row = blockIdx.x * (MID_ROWS >> a.share) + (p.rl >> a.share);
-    p.bz = (blockIdx.y << a.share) + (p.rl & ((1u << a.share) - 1));
+    p.row = row; p.bz = bz;
     p.nt = a.level + c.K;
     p.x = p.nt - 1 - blockIdx.z; p.kt = p.x < a.level ? p.x : c.L + (p.x - a.level);
     p.own = p.x < a.level ? p.x / c.alpha : beta;           // the digit that has x among its own limbs
@@ -151,27 +150,34 @@ __device__ __forceinline__ PosRow pos_row(const DevTables &c, const PosArgs &a, 
     p.limb = (size_t)1 << c.log_n; p.cc = a.pitch * p.limb; p.kc = c.T * p.limb;
     return p;
 }
-// the digits' rows `srow` in shared memory, in order
+// a CTA's warps as MID_ROWS / 2^share rows of 2^share entries
+__device__ __forceinline__ PosRow pos_warp(const DevTables &c, const PosArgs &a, uint32_t beta) {
+    const uint32_t w = threadIdx.x >> 5;
+    return pos_row(c, a, beta, blockIdx.x * (MID_ROWS >> a.share) + (w >> a.share), (blockIdx.y << a.share) + (w & ((1u << a.share) - 1)));
+}
+// row `srow` of digit j at s, in order
+template <uint32_t BETA>
+__device__ __forceinline__ void pos_digit(const DevTables &c, const PosArgs &a, const PosRow &p, const u64 *ct, uint32_t srow, uint32_t j, double *s) {
+    if (j == p.own) {
+        const u64 *d = ct + p.cc + srow * 256 + 2 * p.t;
+        ulonglong2 w[4];
+#pragma unroll
+        for (uint32_t k = 0; k < 4; k++) w[k] = ld_pair<true>(d + 64 * k);
+#pragma unroll
+        for (uint32_t k = 0; k < 4; k++) *reinterpret_cast<double2 *>(s + wrow_at(2 * p.t) + 72 * k) = make_double2(u64_to_d(w[k].x), u64_to_d(w[k].y));
+        return;
+    }
+    const double *g = reinterpret_cast<const double *>(a.ext) + (((size_t)p.bz * BETA + j) * p.nt + p.x) * p.limb + srow * 256 + p.t;
+    double v[8];
+#pragma unroll
+    for (uint32_t k = 0; k < 8; k++) v[k] = g[32 * k];
+    wrow_forward(v, s, p.t, c.twd_fwd + p.kt * p.limb, p.R + srow, p.q, p.qinv);
+}
+// the digits' rows `srow` in shared memory
 template <uint32_t BETA>
 __device__ __forceinline__ void pos_digits(const DevTables &c, const PosArgs &a, const PosRow &p, const u64 *ct, uint32_t srow, double (&sm)[BETA][MID_ROWS][WROW_PAD]) {
 #pragma unroll 1
-    for (uint32_t j = 0; j < BETA; j++) {
-        double *s = sm[j][p.rl];
-        if (j == p.own) {
-            const u64 *d = ct + p.cc + srow * 256 + 2 * p.t;
-            ulonglong2 w[4];
-#pragma unroll
-            for (uint32_t k = 0; k < 4; k++) w[k] = ld_pair<true>(d + 64 * k);
-#pragma unroll
-            for (uint32_t k = 0; k < 4; k++) *reinterpret_cast<double2 *>(s + wrow_at(2 * p.t) + 72 * k) = make_double2(u64_to_d(w[k].x), u64_to_d(w[k].y));
-            continue;
-        }
-        const double *g = reinterpret_cast<const double *>(a.ext) + (((size_t)p.bz * BETA + j) * p.nt + p.x) * p.limb + srow * 256 + p.t;
-        double v[8];
-#pragma unroll
-        for (uint32_t k = 0; k < 8; k++) v[k] = g[32 * k];
-        wrow_forward(v, s, p.t, c.twd_fwd + p.kt * p.limb, p.R + srow, p.q, p.qinv);
-    }
+    for (uint32_t j = 0; j < BETA; j++) pos_digit<BETA>(c, a, p, ct, srow, j, sm[j][p.rl]);
     __syncwarp();
 }
 // e = S_r (<digits, key>_cm + [cm = 0] P sigma_r(c0)) of both components at the words p0 + 64 k, p0 + 64 k + 1: below 1.5 q
@@ -230,7 +236,7 @@ __device__ __forceinline__ void pos_inverse(const DevTables &c, const PosRow &p,
 template <uint32_t BETA>
 __global__ void __launch_bounds__(32 * MID_ROWS, 6) mid_rows_pos(DevTables c, const __grid_constant__ PosArgs a) {
     __shared__ __align__(16) double sm[BETA][MID_ROWS][WROW_PAD];
-    const PosRow p = pos_row(c, a, BETA);
+    const PosRow p = pos_warp(c, a, BETA);
     grid_dep_sync();
     if (p.bz >= a.nb) return;
     const u64 *ct = a.c.at(p.bz) + p.x * p.limb;
@@ -270,7 +276,7 @@ __global__ void __launch_bounds__(32 * MID_ROWS, 6) mid_rows_pos(DevTables c, co
 template <uint32_t BETA>
 __global__ void __launch_bounds__(32 * MID_ROWS, 5) mid_rows_pos_sum(DevTables c, const __grid_constant__ PosArgs a) {
     __shared__ __align__(16) double sm[BETA][MID_ROWS][WROW_PAD];
-    const PosRow p = pos_row(c, a, BETA);
+    const PosRow p = pos_warp(c, a, BETA);
     double s[2][8];
     grid_dep_sync();
     if (p.bz >= a.nb) return;
@@ -310,12 +316,93 @@ __global__ void __launch_bounds__(32 * MID_ROWS, 5) mid_rows_pos_sum(DevTables c
     }
 }
 
+// Five to eight digits: a CTA per row, a warp per digit, then the row's pairs of both components over all threads, because one warp would
+// transform the digits one after the other (one ciphertext at N = 2^13, six digits: 47 us for the call, 41 with launches of their own for the
+// transforms and positions_inner, 37 so; sixteen 116 against 119).  With three digits it is slower from the first ciphertext on at N = 2^16 (180 -> 212
+// us for a token's append) and little faster at N = 2^14 (86 -> 84).
+template <uint32_t BETA>
+__global__ void __launch_bounds__(32 * BETA) mid_rows_pos_wide(DevTables c, const __grid_constant__ PosArgs a) {
+    constexpr uint32_t THREADS = 32 * BETA, ITEMS = (256 + THREADS - 1) / THREADS;
+    __shared__ __align__(16) double sm[BETA][WROW_PAD];
+    const PosRow p = pos_row(c, a, BETA, blockIdx.x, blockIdx.y);
+    double2 acc[ITEMS];                 // item: pair 0 .. 127 of component 0, then of component 1
+    grid_dep_sync();
+    const u64 *ct = a.c.at(p.bz) + p.x * p.limb;
+#pragma unroll
+    for (uint32_t i = 0; i < ITEMS; i++) {
+        const uint32_t w = threadIdx.x + i * THREADS, at = p.row * 256 + 2 * (w & 127), cm = w >> 7;
+        acc[i] = make_double2(0.0, 0.0);
+        if (w >= 256 || p.x >= a.level) continue;
+        const ulonglong2 o = ld_pair<true>(a.own + p.set * a.own_set + p.x * p.limb + at), z = ld_pair<true>(ct + cm * p.cc + at);
+        acc[i] = make_double2(mulmod_dd(mulmod_dd(u64_to_d(z.x), u64_to_d(o.x), p.q, p.qinv), p.pq, p.q, p.qinv),
+                              mulmod_dd(mulmod_dd(u64_to_d(z.y), u64_to_d(o.y), p.q, p.qinv), p.pq, p.q, p.qinv));
+    }
+#pragma unroll 1
+    for (uint32_t r = 0; r < a.nrot; r++) {
+        const uint32_t gal = (uint32_t)a.galois[r];
+        pos_digit<BETA>(c, a, p, ct, galois_src(p.row << 8, gal, c.log_n) >> 8, p.rl, sm[p.rl]);
+        __syncthreads();
+#pragma unroll
+        for (uint32_t i = 0; i < ITEMS; i++) {
+            const uint32_t w = threadIdx.x + i * THREADS, at = p.row * 256 + 2 * (w & 127), cm = w >> 7;
+            if (w >= 256) continue;
+            const uint32_t src = galois_src(at, gal, c.log_n), so = src & 254u;
+            const bool odd = src & 1;                // the permutation maps the pair onto a pair, possibly swapped
+            const u64 *kp = a.evk[r] + cm * p.kc + p.kt * p.limb + at;
+            ulonglong2 kv[BETA];
+#pragma unroll
+            for (uint32_t j = 0; j < BETA; j++) kv[j] = ld_pair<true>(kp + 2 * j * p.kc);
+            const ulonglong2 f = ld_pair<true>(a.fac + r * a.fac_rot + p.set * a.fac_set + p.x * p.limb + at);
+            // as in pos_pair; the sum of c0's product and four digits' is reduced before the others'
+            ProductSum e0, e1;
+            if (cm == 0 && p.x < a.level) {
+                const ulonglong2 z = ld_pair<true>(ct + (src & ~1u));
+                e0.add(u64_to_d(odd ? z.y : z.x), p.pq);
+                e1.add(u64_to_d(odd ? z.x : z.y), p.pq);
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < BETA; j++) {
+                if (j == 4) { e0.carry(p.q, p.qinv); e1.carry(p.q, p.qinv); }
+                const double2 d = *reinterpret_cast<const double2 *>(sm[j] + wrow_at(so));
+                e0.add(odd ? d.y : d.x, u64_to_d(kv[j].x));
+                e1.add(odd ? d.x : d.y, u64_to_d(kv[j].y));
+            }
+            acc[i].x = __dadd_rn(acc[i].x, mulmod_pq<1>(e0.sum(p.q, p.qinv), u64_to_d(f.x), p.q, p.qinv));
+            acc[i].y = __dadd_rn(acc[i].y, mulmod_pq<1>(e1.sum(p.q, p.qinv), u64_to_d(f.y), p.q, p.qinv));
+        }
+        __syncthreads();
+    }
+    u64 *u = a.u + ((size_t)p.bz * 2 * p.nt + p.x) * p.limb + p.row * 256;
+    const bool inverse = p.x >= a.inv_from;
+#pragma unroll
+    for (uint32_t i = 0; i < ITEMS; i++) {
+        const uint32_t w = threadIdx.x + i * THREADS, at = 2 * (w & 127), cm = w >> 7;
+        if (w >= 256) continue;
+        const double x = reduce_d(acc[i].x, p.q, p.qinv), y = reduce_d(acc[i].y, p.q, p.qinv);
+        if (inverse) *reinterpret_cast<double2 *>(sm[cm] + wrow_at(at)) = make_double2(x, y);
+        else st_pair<true>(u + cm * p.nt * p.limb + at, make_ulonglong2(canonical_d(x, p.q), canonical_d(y, p.q)));
+    }
+    if (!inverse) return;
+    __syncthreads();
+    if (p.rl >= 2) return;
+    double v[8];
+    wrow_inverse(v, sm[p.rl], p.t, c.twd_inv + p.kt * p.limb, p.R + p.row, p.q, p.qinv);
+    double *g = reinterpret_cast<double *>(u + p.rl * p.nt * p.limb) + p.t;
+#pragma unroll
+    for (uint32_t k = 0; k < 8; k++) g[32 * k] = v[k];
+}
+
 }  // namespace
 
 void launch_mid_rows_pos(const ckks_ctx *c, const PosArgs &a, uint32_t beta, cudaStream_t s) {
     using K = decltype(&mid_rows_pos<1>);
     static constexpr K one[IP_FUSED_BETA] = {mid_rows_pos<1>, mid_rows_pos<2>, mid_rows_pos<3>, mid_rows_pos<4>};
     static constexpr K sum[IP_FUSED_BETA] = {mid_rows_pos_sum<1>, mid_rows_pos_sum<2>, mid_rows_pos_sum<3>, mid_rows_pos_sum<4>};
+    static constexpr K wide[POS_BETA - IP_FUSED_BETA] = {mid_rows_pos_wide<5>, mid_rows_pos_wide<6>, mid_rows_pos_wide<7>, mid_rows_pos_wide<8>};
+    if (beta > IP_FUSED_BETA) {
+        launch(wide[beta - 1 - IP_FUSED_BETA], dim3(c->N >> 8, a.nb, a.level + c->K), 32 * beta, 0, s, c->dev, a);
+        return;
+    }
     PosArgs b = a;
     b.share = a.nrot > 1 ? 0 : a.nb >= 4 ? 2 : a.nb >= 2 ? 1 : 0;
     const uint32_t e = 1u << b.share;

@@ -16,7 +16,7 @@ from tests.test_oracle_positions import TOL, rotate_clear
 pytestmark = pytest.mark.gpu
 
 SCALE = 2.0 ** 50
-RINGS = {10: (10, 6, 3, 2), 11: (11, 6, 1, 6), 12: (12, 6, 2, 3), 13: (13, 7, 7, 1), 15: (15, 4, 2, 2), 16: (16, 3, 1, 3)}       # log_n: parameters, by ring of the cases
+RINGS = {10: (10, 6, 3, 2), 11: (11, 6, 1, 6), 12: (12, 6, 2, 3), 13: (13, 7, 7, 1), 15: (15, 4, 2, 2), 16: (16, 3, 1, 3), 100: (10, 9, 1, 9)}       # parameters by log_n, or another number for a second set
 
 
 def _ring(log_n):
@@ -131,7 +131,12 @@ CASES = [
     (10, 5, 16, 2, 4, 16, "half", 3, [4, 0, 4], False),                 # copies; two ciphertexts share positions; a partial last digit
     (10, 2, 16, 4, 8, 16, "interleaved", 2, [1, 9], False),             # the smallest level
     (10, 4, 16, 2, 8, 10, "half", 2, [3, 3], True),                     # part of the head, one token in all slots
-    (11, 6, 32, 8, 4, 32, "half", 2, [0, 4], False),                    # six digits: the kernel for any number of them
+    (11, 6, 32, 8, 4, 32, "half", 2, [0, 4], False),                    # six digits
+    (11, 5, 32, 8, 4, 22, "interleaved", 3, [0, 4, 8], False),          # five, two rotations
+    (11, 6, 32, 8, 4, 22, "interleaved", 9, [0, 4, 8, 0, 4, 8, 1, 2, 3], False),     # six, two rotations of many ciphertexts
+    (100, 7, 16, 4, 8, 12, "half", 2, [0, 1], True),                    # seven
+    (100, 8, 16, 4, 8, 16, "half", 17, list(range(17)), False),         # eight
+    (100, 9, 16, 4, 8, 16, "interleaved", 2, [0, 8], False),            # nine: the kernel for any number of them
     (11, 3, 2, 4, 128, 2, "interleaved", 1, [2], False),                # a head of one pair, three digits
     (12, 6, 32, 4, 16, 24, "interleaved", 4, [0, 16, 32, 48], False),
     (12, 3, 64, 32, 1, 64, "half", 19, list(range(19)), False),         # more ciphertexts than run side by side, one token each

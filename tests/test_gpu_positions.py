@@ -16,7 +16,7 @@ from tests.test_oracle_positions import TOL, rotate_clear
 pytestmark = pytest.mark.gpu
 
 SCALE = 2.0 ** 50
-RINGS = {10: (10, 6, 3, 2), 11: (11, 6, 1, 6), 12: (12, 6, 2, 3), 13: (13, 7, 7, 1), 15: (15, 4, 2, 2), 16: (16, 3, 1, 3), 100: (10, 9, 1, 9)}       # parameters by log_n, or another number for a second set
+RINGS = {10: (10, 6, 3, 2), 11: (11, 6, 1, 6), 12: (12, 6, 2, 3), 13: (13, 7, 7, 1), 15: (15, 4, 2, 2), 16: (16, 3, 1, 3), 100: (10, 9, 1, 9), 101: (10, 20, 10, 2)}       # parameters by log_n, or another number for a second set
 
 
 def _ring(log_n):
@@ -136,6 +136,8 @@ CASES = [
     (11, 6, 32, 8, 4, 22, "interleaved", 9, [0, 4, 8, 0, 4, 8, 1, 2, 3], False),     # six, two rotations of many ciphertexts
     (100, 7, 16, 4, 8, 12, "half", 2, [0, 1], True),                    # seven
     (100, 8, 16, 4, 8, 16, "half", 17, list(range(17)), False),         # eight
+    (101, 20, 16, 4, 8, 16, "half", 2, [0, 8], False),                  # digits of ten limbs, ten special primes
+    (101, 11, 16, 4, 8, 14, "half", 3, [2, 0, 2], False),
     (100, 9, 16, 4, 8, 16, "interleaved", 2, [0, 8], False),            # nine: the kernel for any number of them
     (11, 3, 2, 4, 128, 2, "interleaved", 1, [2], False),                # a head of one pair, three digits
     (12, 6, 32, 4, 16, 24, "interleaved", 4, [0, 16, 32, 48], False),
@@ -354,6 +356,7 @@ APPENDS = [
     # log_n, page level, input level, dim, heads, inner, rot, layout, pages in the pool, page numbers, spans
     (10, 3, 4, 16, 4, 8, 16, "half", 1, [0], [(3, 4, 11)]),                                              # one token
     (10, 3, 6, 16, 2, 8, 12, "half", 5, [4, 1, 2], [(0, 8, 0), (0, 8, 8), (0, 3, 16)]),                  # a prompt; inputs of a higher level
+    (101, 19, 20, 16, 4, 8, 16, "half", 2, [1], [(2, 6, 0)]),
     (10, 1, 2, 16, 4, 8, 16, "interleaved", 3, [2, 0], [(7, 8, 0), (1, 7, 5)]),                          # the lowest page level; copies of rows
     (11, 5, 6, 32, 8, 4, 32, "half", 2, [1], [(0, 1, 3)]),                                               # six digits
     (15, 3, 4, 64, 16, 16, 64, "half", 3, [1, 2], [(0, 1, 0), (3, 16, 5)]),                                 # keys and values side by side

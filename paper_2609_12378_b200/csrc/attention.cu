@@ -76,7 +76,7 @@ int check_cts(const ckks_ctx *c, const ckks_ct *cts, uint32_t n, uint32_t *level
 
 bool rlk_ok(const ckks_evk *rlk) { return rlk && rlk->data && rlk->galois == 0; }
 
-uint32_t log2_ceil(uint32_t x) { uint32_t d = 0; while ((1u << d) < x) d++; return d; }
+uint32_t log2_ceil(uint32_t x) { uint32_t d = 0; while ((1ull << d) < x) d++; return d; }
 
 }  // namespace
 
@@ -349,8 +349,8 @@ extern "C" size_t ckks_softmax_rows_workspace_bytes(const ckks_ctx *c, const ckk
 
 // Levels that the Softmax takes from its input, and its levels, scales and constants.  The groups' scales agree within 2^-30 and need not be
 // equal: every u_g has a scale of its own, and the exponential's constants depend on it.
-static uint32_t rows_levels(const ckks_softmax_desc *s, bool masked) {
-    return log2_ceil(s->exp_degree) + 1 + s->rounds * ((s->rounds ? log2_ceil(s->rsqrt_degree) : 0) + 4) + (masked ? 1 : 0);
+static uint64_t rows_levels(const ckks_softmax_desc *s, bool masked) {
+    return log2_ceil(s->exp_degree) + 1 + (uint64_t)s->rounds * ((s->rounds ? log2_ceil(s->rsqrt_degree) : 0) + 4) + (masked ? 1 : 0);
 }
 struct RowsPlan {
     struct Run { uint32_t g0, n; long long shift; TreePlan poly; };       // neighbours of one scale
@@ -626,7 +626,7 @@ static int attend(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc 
     if ((rc = check_cts(c, v, dim_v, &lv, true))) return rc;
     if (maps == 2 && !scales_agree(q[0][0].scale * k[0][0].scale, q[1][0].scale * k[1][0].scale)) return CKKS_ERR_SCALE;
     // scores, Softmax, difference, values
-    const uint32_t lost = 1 + rows_levels(s, mask != nullptr) + (maps - 1);
+    const uint64_t lost = 1 + rows_levels(s, mask != nullptr) + (maps - 1);
     if (level < lost + 2 || lv < level - lost) return CKKS_ERR_LEVEL;
     if (!rlk_ok(rlk)) return CKKS_ERR_NO_KEY;
     for (const std::vector<int64_t> *list : {&p.tok, &p.lad, &p.neg})

@@ -625,6 +625,17 @@ def test_masked_and_differential_attention_refusals():
 
     def diff(q1=q, k1=k, q2=q, k2=k, vv=k, ks=keys, r=rlk, rounds=1, **kw):
         return ctx.attention_differential(q1, k1, q2, k2, vv, w, 0.5, rounds, EXP, [RSQRT] * rounds, r, ks, 8, 2, 4, **kw)
+    S = _dev_cts(_residues(P, 4, 12, desc.groups()))
+    for rounds in (3, 1 << 30, 0xffffffff):              # their levels leave 32 bits
+        poly = binding.Context._softmax_desc(0.5, 1, EXP, [RSQRT])
+        poly.rounds = rounds
+        d = binding.CAttnDesc(8, 2, 4, 1, 1)
+        ca = (binding.CCt * len(S))(*[ctx._ct2(x) for x in S])
+        ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+        for name, extra in (("ckks_softmax_rows", ()), ("ckks_softmax_rows_masked", (C.byref(binding.CAttnMask(1, 0, 8, 0, 0)),))):
+            rc = getattr(binding.load(), name)(ctx._h, C.byref(d), C.byref(poly), *extra, ca, C.byref(binding.CEvk(rlk.data.data_ptr(), 0)), ctx._evks(keys), len(keys), ca,
+                                               ws.data_ptr(), ws.numel(), None)
+            assert rc == binding.ERR_LEVEL, (name, rounds, rc)
     for f in (masked, diff):
         _refused(binding.ERR_NO_KEY, f, ks=keys[:-1])
         _refused(binding.ERR_LEVEL, f, rounds=3)

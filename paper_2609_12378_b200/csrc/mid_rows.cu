@@ -231,31 +231,41 @@ __device__ __forceinline__ void pos_inverse(const DevTables &c, const PosRow &p,
     __syncwarp();
 }
 
-// One rotation: pair by pair, nothing is held from one to the next; the pairs of a limb that is transformed back wait in their place in u.  One
-// ciphertext at level 18: 41 us.
-template <uint32_t BETA>
+// Pair by pair, nothing is held from one to the next: the sums of all rotations but the last (MANY) and the pairs of a limb that is transformed
+// back wait in their place in u.  One ciphertext at level 18: 42 us; two rotations of six at N = 2^15, level 10: 98 us, where sums kept in registers, and
+// five CTAs per SM with them, took 103.
+template <uint32_t BETA, bool MANY>
 __global__ void __launch_bounds__(32 * MID_ROWS, 6) mid_rows_pos(DevTables c, const __grid_constant__ PosArgs a) {
     __shared__ __align__(16) double sm[BETA][MID_ROWS][WROW_PAD];
     const PosRow p = pos_warp(c, a, BETA);
     grid_dep_sync();
     if (p.bz >= a.nb) return;
     const u64 *ct = a.c.at(p.bz) + p.x * p.limb;
-    pos_digits<BETA>(c, a, p, ct, galois_src(p.row << 8, (uint32_t)a.galois[0], c.log_n) >> 8, sm);
     u64 *u0 = a.u + ((size_t)p.bz * 2 * p.nt + p.x) * p.limb + p.row * 256;
     const bool inverse = p.x >= a.inv_from;
+#pragma unroll 1
+    for (uint32_t r = 0; r < (MANY ? a.nrot : 1); r++) {
+        pos_digits<BETA>(c, a, p, ct, galois_src(p.row << 8, (uint32_t)a.galois[r], c.log_n) >> 8, sm);
+        const bool last = !MANY || r + 1 == a.nrot;
 #pragma unroll
-    for (uint32_t k = 0; k < 4; k++) {
-        double2 e[2], o[2];
-        pos_pair<BETA>(c, a, p, ct, 0, k, sm, e);
-        pos_own(a, p, ct, k, o);
+        for (uint32_t k = 0; k < 4; k++) {
+            u64 *u = u0 + 2 * p.t + 64 * k;
+            double2 e[2], o[2];
+            pos_pair<BETA>(c, a, p, ct, r, k, sm, e);
+            if (MANY && r)           // below 1.5 q per rotation
 #pragma unroll
-        for (uint32_t cm = 0; cm < 2; cm++) {
-            const double x = reduce_d(__dadd_rn(e[cm].x, o[cm].x), p.q, p.qinv), y = reduce_d(__dadd_rn(e[cm].y, o[cm].y), p.q, p.qinv);
-            u64 *u = u0 + cm * p.nt * p.limb + 2 * p.t + 64 * k;
-            if (inverse) *reinterpret_cast<double2 *>(u) = make_double2(x, y);
-            else st_pair<true>(u, make_ulonglong2(canonical_d(x, p.q), canonical_d(y, p.q)));
+                for (uint32_t cm = 0; cm < 2; cm++) o[cm] = *reinterpret_cast<const double2 *>(u + cm * p.nt * p.limb);
+            else pos_own(a, p, ct, k, o);
+#pragma unroll
+            for (uint32_t cm = 0; cm < 2; cm++) {
+                double x = __dadd_rn(e[cm].x, o[cm].x), y = __dadd_rn(e[cm].y, o[cm].y);
+                if (last) { x = reduce_d(x, p.q, p.qinv); y = reduce_d(y, p.q, p.qinv); }
+                if (inverse || !last) *reinterpret_cast<double2 *>(u + cm * p.nt * p.limb) = make_double2(x, y);
+                else st_pair<true>(u + cm * p.nt * p.limb, make_ulonglong2(canonical_d(x, p.q), canonical_d(y, p.q)));
+            }
+            asm volatile("" ::: "memory");       // one step's words at a time: the registers hold no more
         }
-        asm volatile("" ::: "memory");       // one step's words at a time: the registers hold no more
+        if (MANY) __syncwarp();
     }
     if (!inverse) return;
 #pragma unroll 1
@@ -268,51 +278,6 @@ __global__ void __launch_bounds__(32 * MID_ROWS, 6) mid_rows_pos(DevTables c, co
         }
         __syncwarp();
         pos_inverse(c, p, v, sm[0][p.rl], reinterpret_cast<double *>(u0));
-    }
-}
-
-// Several rotations: their sums stay in registers, five CTAs per SM (two rotations of six ciphertexts at N = 2^15, level 10: 103 us; with ciphertexts
-// sharing a CTA 131: six do not fill the groups of four)
-template <uint32_t BETA>
-__global__ void __launch_bounds__(32 * MID_ROWS, 5) mid_rows_pos_sum(DevTables c, const __grid_constant__ PosArgs a) {
-    __shared__ __align__(16) double sm[BETA][MID_ROWS][WROW_PAD];
-    const PosRow p = pos_warp(c, a, BETA);
-    double s[2][8];
-    grid_dep_sync();
-    if (p.bz >= a.nb) return;
-    const u64 *ct = a.c.at(p.bz) + p.x * p.limb;
-#pragma unroll
-    for (uint32_t k = 0; k < 4; k++) {
-        double2 o[2];
-        pos_own(a, p, ct, k, o);
-#pragma unroll
-        for (uint32_t cm = 0; cm < 2; cm++) { s[cm][2 * k] = o[cm].x; s[cm][2 * k + 1] = o[cm].y; }
-    }
-#pragma unroll 1
-    for (uint32_t r = 0; r < a.nrot; r++) {
-        pos_digits<BETA>(c, a, p, ct, galois_src(p.row << 8, (uint32_t)a.galois[r], c.log_n) >> 8, sm);
-#pragma unroll
-        for (uint32_t k = 0; k < 4; k++) {
-            double2 e[2];
-            pos_pair<BETA>(c, a, p, ct, r, k, sm, e);
-#pragma unroll
-            for (uint32_t cm = 0; cm < 2; cm++) {           // below 0.75 q and 1.5 q per rotation
-                s[cm][2 * k] = __dadd_rn(s[cm][2 * k], e[cm].x);
-                s[cm][2 * k + 1] = __dadd_rn(s[cm][2 * k + 1], e[cm].y);
-            }
-            asm volatile("" ::: "memory");
-        }
-        __syncwarp();
-    }
-    u64 *u = a.u + ((size_t)p.bz * 2 * p.nt + p.x) * p.limb + p.row * 256;
-#pragma unroll
-    for (uint32_t cm = 0; cm < 2; cm++, u += p.nt * p.limb) {
-#pragma unroll
-        for (uint32_t k = 0; k < 8; k++) s[cm][k] = reduce_d(s[cm][k], p.q, p.qinv);
-        if (p.x >= a.inv_from) { pos_inverse(c, p, s[cm], sm[0][p.rl], reinterpret_cast<double *>(u)); continue; }
-#pragma unroll
-        for (uint32_t k = 0; k < 4; k++)
-            st_pair<true>(u + 2 * p.t + 64 * k, make_ulonglong2(canonical_d(s[cm][2 * k], p.q), canonical_d(s[cm][2 * k + 1], p.q)));
     }
 }
 
@@ -395,18 +360,18 @@ __global__ void __launch_bounds__(32 * BETA) mid_rows_pos_wide(DevTables c, cons
 }  // namespace
 
 void launch_mid_rows_pos(const ckks_ctx *c, const PosArgs &a, uint32_t beta, cudaStream_t s) {
-    using K = decltype(&mid_rows_pos<1>);
-    static constexpr K one[IP_FUSED_BETA] = {mid_rows_pos<1>, mid_rows_pos<2>, mid_rows_pos<3>, mid_rows_pos<4>};
-    static constexpr K sum[IP_FUSED_BETA] = {mid_rows_pos_sum<1>, mid_rows_pos_sum<2>, mid_rows_pos_sum<3>, mid_rows_pos_sum<4>};
+    using K = decltype(&mid_rows_pos<1, false>);
+    static constexpr K one[IP_FUSED_BETA] = {mid_rows_pos<1, false>, mid_rows_pos<2, false>, mid_rows_pos<3, false>, mid_rows_pos<4, false>};
+    static constexpr K many[IP_FUSED_BETA] = {mid_rows_pos<1, true>, mid_rows_pos<2, true>, mid_rows_pos<3, true>, mid_rows_pos<4, true>};
     static constexpr K wide[POS_BETA - IP_FUSED_BETA] = {mid_rows_pos_wide<5>, mid_rows_pos_wide<6>, mid_rows_pos_wide<7>, mid_rows_pos_wide<8>};
     if (beta > IP_FUSED_BETA) {
         launch(wide[beta - 1 - IP_FUSED_BETA], dim3(c->N >> 8, a.nb, a.level + c->K), 32 * beta, 0, s, c->dev, a);
         return;
     }
     PosArgs b = a;
-    b.share = a.nrot > 1 ? 0 : a.nb >= 4 ? 2 : a.nb >= 2 ? 1 : 0;
+    b.share = a.nb % 4 == 0 || a.nb > 12 ? 2 : a.nb % 2 == 0 || a.nb > 4 ? 1 : 0;        // few idle warps: groups that the entries fill, or many groups
     const uint32_t e = 1u << b.share;
-    launch((a.nrot > 1 ? sum : one)[beta - 1], dim3((c->N >> 8) / (MID_ROWS >> b.share), (a.nb + e - 1) / e, a.level + c->K), 32 * MID_ROWS, 0, s, c->dev, b);
+    launch((a.nrot > 1 ? many : one)[beta - 1], dim3((c->N >> 8) / (MID_ROWS >> b.share), (a.nb + e - 1) / e, a.level + c->K), 32 * MID_ROWS, 0, s, c->dev, b);
 }
 void launch_mid_rows(const ckks_ctx *c, const MidArgs &a, uint32_t beta, cudaStream_t s) {
     using K = decltype(&mid_rows<1, false>);

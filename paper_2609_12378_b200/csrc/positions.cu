@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "common.cuh"
+#include "frequencies.cuh"
 
 namespace {
 
@@ -22,9 +23,10 @@ constexpr uint32_t THREADS = 256;
 
 // ---- the table of angles --------------------------------------------------------------------------------------------
 constexpr uint32_t ROT_MAX = 256;
-struct Turns { double hi[ROT_MAX / 2], lo[ROT_MAX / 2]; };      // angle per position over pi, as an unevaluated sum
+struct Turns { double hi[ROT_MAX / 2], lo[ROT_MAX / 2]; };      // angle per position over pi, as an unevaluated sum (frequencies.cuh)
 
-// The angle over pi is formed as a sum of two doubles and reduced exactly, so that far positions lose nothing.
+// The angle over pi is formed as a sum of two doubles and reduced exactly, so that far positions lose nothing.  A unit is off by less
+// than 3 * 2^-52: by its argument's rounding, at most pi 2^-53, and by two units in the last place of each of its values.
 __device__ __forceinline__ double2 unit(double pos, double w_hi, double w_lo) {
     const double hi = __dmul_rn(pos, w_hi), lo = __fma_rn(pos, w_lo, __fma_rn(pos, w_hi, -hi));
     const double r = __dsub_rn(hi, __dmul_rn(2.0, rint(__dmul_rn(0.5, hi))));
@@ -33,8 +35,8 @@ __device__ __forceinline__ double2 unit(double pos, double w_hi, double w_lo) {
     return make_double2(c, s);
 }
 // cos, sin [count][half] of position first + row, a CTA per R^2 rows and 32 columns: R + R units per column from the functions, the others
-// as products e^(i w (base + offset)), four operations where the function takes tens.  Their error is that of two units and one product,
-// below 3 * 2^-52.  Bound by its stores from R = 16 on: 131072 positions of 64 pairs, 134 MB, in 25.6 us (5.2 TB/s; 121 us with every value from the function).
+// as products e^(i w (base + offset)), four operations where the function takes tens.  Their error is that of two units, of the
+// magnitude's product and of their own: below 7 * 2^-52 times the magnitude, and 2^-52 from the frequency at position 2^50.  Bound by its stores from R = 16 on: 131072 positions of 64 pairs, 134 MB, in 25.6 us (5.2 TB/s; 121 us with every value from the function).
 template <uint32_t R>
 __global__ void __launch_bounds__(THREADS) rotary_table_kernel(const __grid_constant__ Turns w, uint64_t first, uint64_t count, uint32_t half, double magnitude,
                                                              double *cosv, double *sinv) {
@@ -300,27 +302,8 @@ extern "C" int32_t ckks_rotary_table(ckks_ctx *c, const ckks_rotary_scaling *f, 
     if ((f->rot_dim & 1) || f->rot_dim > ROT_MAX || (f->kind == CKKS_ROTARY_BASE && f->rot_dim < 4)) return CKKS_ERR_UNSUPPORTED;
     // positions are exact in doubles, and so are their products' high parts once reduced
     if (first > (1ull << 50) || count > (1ull << 38) || first + count > (1ull << 50)) return CKKS_ERR_UNSUPPORTED;
-    const double rot = f->rot_dim, theta = f->kind == CKKS_ROTARY_BASE ? f->theta * pow(f->factor, rot / (rot - 2.0)) : f->theta;
-    // 1 / pi as a sum of two doubles
-    const double ipi_hi = 0.318309886183790671538, ipi_lo = -1.96786766751824869e-17;
-    double ramp_lo = 0.0, ramp_hi = 0.0;
-    if (f->kind == CKKS_ROTARY_RAMP) {          // pair index at which a wavelength turns `many`, `few` times within the trained length
-        ramp_lo = fmax(0.0, floor(rot * log(f->original_length / (many * 2.0 * M_PI)) / (2.0 * log(theta))));
-        ramp_hi = fmin(rot - 1.0, ceil(rot * log(f->original_length / (few * 2.0 * M_PI)) / (2.0 * log(theta))));
-    }
-    Turns w{};
-    for (uint32_t j = 0; j < f->rot_dim / 2; j++) {
-        double a = pow(theta, -2.0 * (double)j / rot);
-        if (f->kind == CKKS_ROTARY_LINEAR) a /= f->factor;
-        if (by_turns) {
-            const double turns = f->original_length * a / (2.0 * M_PI);
-            const double keep = f->kind == CKKS_ROTARY_BANDS ? (turns - few) / (many - few) : 1.0 - fmin(1.0, fmax(0.0, ((double)j - ramp_lo) / fmax(ramp_hi - ramp_lo, 0.001)));
-            const double k = fmin(1.0, fmax(0.0, keep));
-            a = k * a + (1.0 - k) * (a / f->factor);
-        }
-        w.hi[j] = a * ipi_hi;
-        w.lo[j] = fma(a, ipi_hi, -w.hi[j]) + a * ipi_lo;
-    }
+    Turns w;
+    rotary_frequencies(*f, few, many, w.hi, w.lo);
     const uint32_t half = f->rot_dim / 2, cols = (half + 31) / 32;
     const double mag = f->magnitude == 0.0 ? 1.0 : f->magnitude;
     DeviceGuard guard(c->device);

@@ -1,0 +1,62 @@
+"""GPU parity of positions, cache pages, masks and differences where the other file's shapes do not reach: far positions of every pair, calls large
+enough for the kernels of large calls, buffers of eight-byte alignment, and what the calls refuse."""
+import math
+from decimal import Decimal
+
+import numpy as np
+import pytest
+
+from paper_2609_12378_b200 import binding
+from tests.test_frequencies_host import PI, angles
+from tests.test_gpu_positions import _ring
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- the table -------------------------------------------------------------------------------------------------------
+def _unit(position, w):
+    """cos, sin of position * w as Decimals good to 2^-100: a double's functions at the angle's nearest double, and the rest's first order."""
+    a = position * w % (2 * PI)
+    if a > PI:
+        a -= 2 * PI
+    r = float(a)
+    rest = a - Decimal(r)                     # below 2^-52: its square is left out, the functions at r are exact to 2^-53
+    c, s = Decimal(math.cos(r)), Decimal(math.sin(r))
+    return c - rest * s, s + rest * c
+
+
+@pytest.mark.parametrize("rot,theta", [(128, 500000.0), (96, 10000.0), (256, 1.5)])
+@pytest.mark.parametrize("kind,factor", [("none", 1.0), ("linear", 3.0), ("base", 8.0), ("bands", 8.0), ("ramp", 32.0)])
+def test_every_pair_of_a_far_position_is_as_exact_as_of_a_near_one(rot, theta, kind, factor):
+    """A unit is off by less than 3 * 2^-52 (the rounding of its argument, at most pi 2^-53, and two units in the last place of each value), a value by two
+    units, the magnitude's product and its own, 7 * 2^-52, and by the frequency's 2^-103 relative times the position, 2^-52 at most: 2^-49
+    in all, times the magnitude; the comparison's own functions add 2^-53."""
+    _, ctx = _ring(10)
+    few, many = (1.0, 4.0) if kind == "bands" else (1.0, 32.0)
+    w = angles(rot, theta, kind, factor, 8192.0, few, many)
+    pairs = sorted({0, 1, 2, 5, rot // 8, rot // 4, rot // 2 - 1})
+    for first in (0, (1 << 20) + 3, (1 << 36) - 7, (1 << 50) - 9):
+        cos, sin = (t.cpu().numpy() for t in ctx.rotary_table(rot, first, 9, theta=theta, scaling=kind, factor=factor, original_length=8192.0, magnitude=1.25))
+        for i in (0, 3, 8):
+            for j in pairs:
+                c, s = _unit(Decimal(first + i), w[j])
+                for got, want in ((cos[i, j], c), (sin[i, j], s)):
+                    assert abs(Decimal(float(got)) - Decimal(1.25) * want) <= Decimal(1.25) * (Decimal(2) ** -49 + Decimal(2) ** -53), (first + i, j, got)
+
+
+def test_a_long_table_of_an_odd_shape():
+    """Enough rows for the large tiles, the last one cut, and columns that fill no tile: sampled rows, the last ones among them, against the same
+    positions' rows of short tables and the definition."""
+    _, ctx = _ring(10)
+    rot, first, count = 70, 1000003, 131072 * 2 + 77                     # 35 pairs: two column tiles; 1025 row tiles of 256
+    cos, sin = (t.cpu().numpy() for t in ctx.rotary_table(rot, first, count, theta=10000.0))
+    w = angles(rot, 10000.0, "none", 1.0, 0.0, 1.0, 4.0)
+    assert cos.shape == (count, rot // 2)
+    for i in (0, 1, 15, 16, 255, 256, 4095, 77777, count - 78, count - 77, count - 2, count - 1):
+        for j in (0, 1, 31, 32, 33, 34):
+            c, s = _unit(Decimal(first + i), w[j])
+            assert abs(Decimal(float(cos[i, j])) - c) <= Decimal(2) ** -49 + Decimal(2) ** -53, (i, j)
+            assert abs(Decimal(float(sin[i, j])) - s) <= Decimal(2) ** -49 + Decimal(2) ** -53, (i, j)
+    near = ctx.rotary_table(rot, first + count - 5, 5, theta=10000.0)
+    for got, want in zip((cos[-5:], sin[-5:]), near):
+        assert np.abs(got - want.cpu().numpy()).max() <= 2.0 ** -48

@@ -382,7 +382,8 @@ size_t ckks_attention_workspace_bytes(const ckks_ctx *ctx, const ckks_attn_desc 
  *     Workspace: ckks_softmax_rows_workspace_bytes.
  *   ckks_attention_masked: ckks_attention with that Softmax.
  *   ckks_attention_differential: the values under softmax(q1 k1) - W softmax(q2 k2), both maps masked if mask is not null: the two maps' scores
- *     and Softmax, ckks_attention_difference, ckks_attention_values.  All operands at one level; the two maps' score scales within 2^-30.
+ *     and Softmax, ckks_attention_difference, ckks_attention_values.  All operands at one level; the two maps' score scales within 2^-30,
+ *     and those of their probabilities too, which drift apart by some twenty times per round.
  *     Levels: one more than ckks_attention (two with a mask).
  * Results may not lie on inputs or on each other (ckks_attention_masked and _differential: as ckks_attention).  These calls check and plan
  * everything before the first launch.  Errors: ARG (key_begin > key_end, key_end > tokens, |query_offset| > 2^31, overlaps), LEVEL, SCALE,

@@ -641,6 +641,8 @@ static int attend(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc 
         const std::vector<double> scales(p.G, q[m][0].scale * k[m][0].scale / (double)c->mod[level - 1]);
         if ((rc = rows_plan(c, p, s, scales, level - 1, mask != nullptr, plan[m]))) return rc;
     }
+    for (uint32_t g = 0; g < p.G && maps == 2; g++)       // the rounds take a difference of the scores' scales to many times itself
+        if (!scales_agree(plan[0].su[g], plan[1].su[g])) return CKKS_ERR_SCALE;
     char *base = (char *)ws;
     auto map = [&](uint32_t m) {
         std::vector<ckks_ct> x(p.G);

@@ -6,9 +6,11 @@ from decimal import Decimal
 import numpy as np
 import pytest
 
+from oracle.ckks_oracle import AttnDesc
 from paper_2609_12378_b200 import binding
+from tests.harness import params
 from tests.test_frequencies_host import PI, angles
-from tests.test_gpu_positions import _ring
+from tests.test_gpu_positions import EXP, RSQRT, SCALE, _dev_cts, _dev_keys, _keys, _refused, _residues, _ring
 
 pytestmark = pytest.mark.gpu
 
@@ -60,3 +62,27 @@ def test_a_long_table_of_an_odd_shape():
     near = ctx.rotary_table(rot, first + count - 5, 5, theta=10000.0)
     for got, want in zip((cos[-5:], sin[-5:]), near):
         assert np.abs(got - want.cpu().numpy()).max() <= 2.0 ** -48
+
+
+# ---- scales of two maps ------------------------------------------------------------------------------------------------------
+def test_maps_whose_scales_part_in_the_softmax_are_refused():
+    """A round takes a relative difference of the scales to about twenty times itself (u^2 and the polynomial of degree 2 in its square, times u, squared):
+    scores just within 2^-30 of each other leave probabilities that may not be subtracted."""
+    import torch
+    from tests.gpu_util import context, key_dev
+    P, ctx = params(10, 13, 4, 4), context(10, 13, 4, 4)
+    o, desc = P.oracle, AttnDesc(8, 2, 4)
+    tok, lad = o.attention_rotations(desc)
+    keys, rlk = _dev_keys(_keys(P, 5, tok + lad)), key_dev(_keys(P, 6, [0]).popitem()[1], 0)
+    q, k = _dev_cts(_residues(P, 1, 13, 2)), _dev_cts(_residues(P, 2, 13, 2))
+    w = torch.ones(2, dtype=torch.float64, device="cuda")
+
+    def diff(off, rounds, **kw):
+        q2 = _dev_cts(_residues(P, 3, 13, 2), SCALE * (1 + off))
+        return ctx.attention_differential(q, k, q2, k, k, w, 0.5, rounds, EXP, [RSQRT] * rounds, rlk, keys, 8, 2, 4, **kw)
+    launches = binding.kernel_launches()
+    for kw in (dict(), dict(masked=True, causal=True)):
+        _refused(binding.ERR_SCALE, diff, 0.9 * 2.0 ** -30, 1, **kw)
+        _refused(binding.ERR_SCALE, diff, -0.2 * 2.0 ** -30, 1, **kw)
+    assert binding.kernel_launches() == launches
+    assert len(diff(2.0 ** -36, 1)) == 2

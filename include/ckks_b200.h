@@ -385,9 +385,9 @@ size_t ckks_attention_workspace_bytes(const ckks_ctx *ctx, const ckks_attn_desc 
  *     and Softmax, ckks_attention_difference, ckks_attention_values.  All operands at one level; the two maps' score scales within 2^-30,
  *     and those of their probabilities too, which drift apart by some twenty times per round.
  *     Levels: one more than ckks_attention (two with a mask).
- * Results may not lie on inputs or on each other (ckks_attention_masked and _differential: as ckks_attention).  These calls check and plan
- * everything before the first launch.  Errors: ARG (key_begin > key_end, key_end > tokens, |query_offset| > 2^31, overlaps), LEVEL, SCALE,
- * NO_KEY, WORKSPACE, UNSUPPORTED, RANGE as above. */
+ * Results and the workspace may not lie on inputs, weights or each other (ckks_softmax_rows_masked, ckks_attention_masked and _differential: as
+ * the calls without a mask, which do not check it).  These calls check and plan everything before the first launch.  Errors: ARG (key_begin >
+ * key_end, key_end > tokens, |query_offset| > 2^31, overlaps), LEVEL, SCALE, NO_KEY, WORKSPACE, UNSUPPORTED, RANGE as above. */
 typedef struct { uint32_t causal, key_begin, key_end, window; int64_t query_offset; } ckks_attn_mask;
 int32_t ckks_attention_mask(ckks_ctx *ctx, const ckks_attn_desc *desc, const ckks_attn_mask *mask, const ckks_ct *in, ckks_ct *out, void *ws,
                             size_t ws_bytes, void *stream);
@@ -439,9 +439,9 @@ size_t ckks_attention_differential_workspace_bytes(const ckks_ctx *ctx, const ck
  *     inputs at one level above it per side, of which l + 1 limbs are read; the scales of inputs and pages agree within 2^-30.  A page may be named
  *     once.  Keys and values of a page written by ckks_cache_append go to ckks_attention_pack as they are, with ckks_attn_mask's key_end at
  *     the number of tokens.
- * Written buffers may not overlap each other or anything that is read, but for a page in place.  Errors: ARG (also a table row past table_rows, a
- * page number past npages, an empty span), LEVEL, SCALE, NO_KEY, WORKSPACE, UNSUPPORTED (dim * heads * token_inner does not divide n, rot_dim odd or
- * above dim).  Tables are read when the kernels run; values beyond the encoder's range set ckks_encode_range_flag. */
+ * Written buffers (the workspace is one) may not overlap each other or anything that is read (tables and keys too), but for a page in place.
+ * Errors: ARG (also a table row past table_rows, a page number past npages, an empty span), LEVEL, SCALE, NO_KEY, WORKSPACE, UNSUPPORTED (dim *
+ * heads * token_inner does not divide n, rot_dim odd or above dim).  Tables are read when the kernels run; values beyond the encoder's range set ckks_encode_range_flag. */
 enum { CKKS_ROTARY_HALF = 0, CKKS_ROTARY_INTERLEAVED = 1 };
 enum { CKKS_ROTARY_PLAIN = 0, CKKS_ROTARY_LINEAR = 1, CKKS_ROTARY_BASE = 2, CKKS_ROTARY_BANDS = 3, CKKS_ROTARY_RAMP = 4 };
 typedef struct { int32_t kind; uint32_t rot_dim; double theta, factor, original_length, turns_few, turns_many, magnitude; } ckks_rotary_scaling;

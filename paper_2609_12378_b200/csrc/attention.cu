@@ -255,10 +255,13 @@ static void difference_groups(const ckks_ctx *c, const AttnPlan &p, const double
         launch_plain_rescale(c, a, (u64 *)rest, s, nb);
     }
 }
-// results may not lie on inputs or on each other
-static bool results_apart(const ckks_ctx *c, uint32_t level, const ckks_ct *const *in, uint32_t nin, const ckks_ct *out, uint32_t G) {
+// results and the workspace may not lie on inputs, weights (may be null) or each other
+static bool results_apart(const ckks_ctx *c, uint32_t level, const ckks_ct *const *in, uint32_t nin, const double *weights, uint32_t heads, const ckks_ct *out, uint32_t G,
+                          const void *ws, size_t ws_bytes) {
     const size_t bi = (size_t)2 * level * c->N * sizeof(u64), bo = (size_t)2 * (level - 1) * c->N * sizeof(u64);
     Buffers buffers;
+    if (weights) buffers.read(weights, heads * sizeof(double));
+    buffers.write(ws, ws_bytes);
     for (uint32_t g = 0; g < G; g++) {
         for (uint32_t x = 0; x < nin; x++) buffers.read(in[x][g].data, bi);
         buffers.write(out[g].data, bo);
@@ -285,8 +288,9 @@ extern "C" int32_t ckks_attention_mask(ckks_ctx *c, const ckks_attn_desc *d, con
         if (level < 2) return CKKS_ERR_LEVEL;
         for (uint32_t g = 0; g < p.G; g++)
             if (!out[g].data) return CKKS_ERR_ARG;
-        if (!results_apart(c, level, &in, 1, out, p.G)) return CKKS_ERR_ARG;
-        if (!ws || ws_bytes < ckks_attention_mask_workspace_bytes(c, d, level)) return CKKS_ERR_WORKSPACE;
+        const size_t need = ckks_attention_mask_workspace_bytes(c, d, level);
+        if (!ws || ws_bytes < need) return CKKS_ERR_WORKSPACE;
+        if (!results_apart(c, level, &in, 1, nullptr, 0, out, p.G, ws, need)) return CKKS_ERR_ARG;
         std::vector<const u64 *> vi;
         std::vector<u64 *> vo;
         for (uint32_t g = 0; g < p.G; g++) { vi.push_back((const u64 *)in[g].data); vo.push_back((u64 *)out[g].data); }
@@ -319,8 +323,9 @@ extern "C" int32_t ckks_attention_difference(ckks_ctx *c, const ckks_attn_desc *
             if (!scales_agree(x[g].scale, y[g].scale)) return CKKS_ERR_SCALE;
         }
         const ckks_ct *ins[2] = {x, y};
-        if (!results_apart(c, level, ins, 2, out, p.G)) return CKKS_ERR_ARG;
-        if (!ws || ws_bytes < ckks_attention_difference_workspace_bytes(c, d, level)) return CKKS_ERR_WORKSPACE;
+        const size_t need = ckks_attention_difference_workspace_bytes(c, d, level);
+        if (!ws || ws_bytes < need) return CKKS_ERR_WORKSPACE;
+        if (!results_apart(c, level, ins, 2, weights, p.H, out, p.G, ws, need)) return CKKS_ERR_ARG;
         DeviceGuard guard(c->device);
         difference_groups(c, p, weights, x, y, out, level, ws, (cudaStream_t)stream);
         rc = finish(c);

@@ -289,6 +289,15 @@ void append_items(ckks_ctx *c, uint32_t token_inner, const std::vector<Item> &it
     }
 }
 
+// what the rotation reads besides its ciphertexts
+void read_factors(const ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, const double *cosv, const double *sinv, uint32_t table_rows, const ckks_evk *keys,
+                  uint32_t nkeys, Buffers &b) {
+    const size_t table = (size_t)table_rows * (d->rot_dim / 2) * sizeof(double);
+    b.read(cosv, table);
+    b.read(sinv, table);
+    for (uint32_t r = 0; r < p.nrot; r++) b.read(find_key(c, keys, nkeys, p.rots[r])->data, (size_t)c->dnum * 2 * c->T * c->N * sizeof(u64));
+}
+
 }  // namespace
 
 extern "C" int32_t ckks_rotary_table(ckks_ctx *c, const ckks_rotary_scaling *f, uint64_t first, uint64_t count, double *cosv, double *sinv, void *stream) {
@@ -302,6 +311,8 @@ extern "C" int32_t ckks_rotary_table(ckks_ctx *c, const ckks_rotary_scaling *f, 
     if ((f->rot_dim & 1) || f->rot_dim > ROT_MAX || (f->kind == CKKS_ROTARY_BASE && f->rot_dim < 4)) return CKKS_ERR_UNSUPPORTED;
     // positions are exact in doubles, and so are their products' high parts once reduced
     if (first > (1ull << 50) || count > (1ull << 38) || first + count > (1ull << 50)) return CKKS_ERR_UNSUPPORTED;
+    const uintptr_t bytes = count * (f->rot_dim / 2) * sizeof(double), pc = (uintptr_t)cosv, ps = (uintptr_t)sinv;
+    if (pc < ps + bytes && ps < pc + bytes) return CKKS_ERR_ARG;
     Turns w;
     rotary_frequencies(*f, few, many, w.hi, w.lo);
     const uint32_t half = f->rot_dim / 2, cols = (half + 31) / 32;
@@ -346,12 +357,15 @@ extern "C" int32_t ckks_rotary(ckks_ctx *c, const ckks_rotary_desc *d, const ckk
         for (uint32_t i = 1; i < n; i++)
             if (in[i].level != level) return CKKS_ERR_LEVEL;
         const size_t bi = (size_t)2 * level * c->N * sizeof(u64), bo = (size_t)2 * (level - 1) * c->N * sizeof(u64);
-        Buffers buffers;
-        for (uint32_t i = 0; i < n; i++) { buffers.read(in[i].data, bi); buffers.write(out[i].data, bo); }
-        if (!buffers.apart()) return CKKS_ERR_ARG;
         for (uint32_t r = 0; r < p.nrot; r++)
             if (!find_key(c, keys, nkeys, p.rots[r])) return CKKS_ERR_NO_KEY;
-        if (!ws || ws_bytes < rotary_bytes(c, level, p.nrot, false, std::min(n, KS_MULTI))) return CKKS_ERR_WORKSPACE;
+        const size_t need = rotary_bytes(c, level, p.nrot, false, std::min(n, KS_MULTI));
+        if (!ws || ws_bytes < need) return CKKS_ERR_WORKSPACE;
+        Buffers buffers;
+        for (uint32_t i = 0; i < n; i++) { buffers.read(in[i].data, bi); buffers.write(out[i].data, bo); }
+        read_factors(c, d, p, cosv, sinv, table_rows, keys, nkeys, buffers);
+        buffers.write(ws, need);
+        if (!buffers.apart()) return CKKS_ERR_ARG;
         std::vector<Item> items;
         for (uint32_t i = 0; i < n; i++) items.push_back(Item{(const u64 *)in[i].data, nullptr, (u64 *)out[i].data, rows[i], 0, d->token_inner});
         DeviceGuard guard(c->device);
@@ -406,7 +420,10 @@ extern "C" int32_t ckks_cache_append(ckks_ctx *c, const ckks_rotary_desc *d, con
             for (uint32_t i = 0; i < n; i++)
                 if (!scales_agree(sd.in[i].scale, sd.page[pages[i]].scale)) return CKKS_ERR_SCALE;
         }
-        const size_t bp = (size_t)2 * level * c->N * sizeof(u64);
+        for (uint32_t r = 0; r < p.nrot && rotated; r++)
+            if (!find_key(c, keys, nkeys, p.rots[r])) return CKKS_ERR_NO_KEY;
+        const size_t bp = (size_t)2 * level * c->N * sizeof(u64), need = ckks_cache_append_workspace_bytes(c, d, level, n);
+        if (!ws || ws_bytes < need) return CKKS_ERR_WORKSPACE;
         Buffers buffers;
         for (const Side &sd : sides)
             for (uint32_t i = 0; i < n; i++) {
@@ -415,10 +432,9 @@ extern "C" int32_t ckks_cache_append(ckks_ctx *c, const ckks_rotary_desc *d, con
                 if (pg != o) buffers.read(pg, bp);
                 buffers.write(o, bp);
             }
+        if (rotated) read_factors(c, d, p, cosv, sinv, table_rows, keys, nkeys, buffers);
+        buffers.write(ws, need);
         if (!buffers.apart()) return CKKS_ERR_ARG;
-        for (uint32_t r = 0; r < p.nrot && rotated; r++)
-            if (!find_key(c, keys, nkeys, p.rots[r])) return CKKS_ERR_NO_KEY;
-        if (!ws || ws_bytes < ckks_cache_append_workspace_bytes(c, d, level, n)) return CKKS_ERR_WORKSPACE;
         DeviceGuard guard(c->device);
         std::vector<std::vector<Item>> items(sides.size());
         for (size_t x = 0; x < sides.size(); x++)

@@ -86,3 +86,76 @@ def test_maps_whose_scales_part_in_the_softmax_are_refused():
         _refused(binding.ERR_SCALE, diff, -0.2 * 2.0 ** -30, 1, **kw)
     assert binding.kernel_launches() == launches
     assert len(diff(2.0 ** -36, 1)) == 2
+
+
+# ---- buffers on one another ----------------------------------------------------------------------------------------------------
+def test_a_table_s_halves_may_not_overlap():
+    import torch
+    _, ctx = _ring(10)
+    buf = torch.zeros(33 * 8, dtype=torch.float64, device="cuda")
+    at = lambda x: buf[8 * x: 8 * x + 128].view(16, 8)  # noqa: E731
+    launches = binding.kernel_launches()
+    for a, b in ((0, 0), (0, 15), (15, 0), (3, 4)):
+        _refused(binding.ERR_ARG, ctx.rotary_table, 16, 0, 16, out=(at(a), at(b)))
+    assert binding.kernel_launches() == launches
+    ctx.rotary_table(16, 0, 16, out=(at(16), at(0)))          # neighbours
+
+
+def _as_table(t, rows, half):
+    import torch
+    return t.view(-1)[:rows * half].view(torch.float64).view(rows, half)
+
+
+def test_calls_on_tables_keys_weights_or_workspaces_in_their_results_place_are_refused():
+    import torch
+    P, ctx = _ring(10)
+    a, level = (16, 4, 8), 4
+    C = lambda t, s=SCALE: binding.Ciphertext(t, s)  # noqa: E731
+    x, v = _dev_cts(_residues(P, 1, level, 1)), _dev_cts(_residues(P, 2, level, 1))
+    pk, pv = _dev_cts(_residues(P, 3, level - 1, 1)), _dev_cts(_residues(P, 4, level - 1, 1))
+    keys = _dev_keys(_keys(P, 2, P.oracle.rotary_rotations(*a, 16, False)))
+    cos, sin = ctx.rotary_table(16, 0, 8)
+    out = [C(torch.empty((2, level - 1, P.N), dtype=torch.uint64, device="cuda"))]
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    on_ws = lambda shape: ws[4096: 4096 + 8 * int(np.prod(shape))].view(torch.uint64).view(shape)  # noqa: E731
+    launches = binding.kernel_launches()
+
+    def rotary(**kw):
+        kw = dict(cts=x, cos=cos, sin=sin, keys=keys, outs=out, ws=ws) | kw
+        return ctx.rotary(kw["cts"], [0], kw["cos"], kw["sin"], kw["keys"], *a, outs=kw["outs"], ws=kw["ws"])
+
+    def append(**kw):
+        kw = dict(k=x, v=v, pk=pk, pv=pv, cos=cos, sin=sin, keys=keys, ws=ws, out_k=None) | kw
+        return ctx.cache_append(kw["k"], kw["v"], [0], [(1, 3, 0)], kw["pk"], kw["pv"], kw["cos"], kw["sin"], kw["keys"], *a, out_k=kw["out_k"], ws=kw["ws"])
+    key_ws = [binding.SwitchKey(on_ws(tuple(k.data.shape)), k.galois) for k in keys]
+    on_key = lambda l: [C(keys[0].data.view(-1)[:2 * l * P.N].view(2, l, P.N))]  # noqa: E731
+    for name in ("cos", "sin"):
+        _refused(binding.ERR_ARG, rotary, **{name: _as_table(out[0].data, 8, 8)})
+        _refused(binding.ERR_ARG, rotary, **{name: _as_table(on_ws((64,)), 8, 8)})
+        _refused(binding.ERR_ARG, append, **{name: _as_table(pk[0].data, 8, 8)})
+        _refused(binding.ERR_ARG, append, **{name: _as_table(pv[0].data, 8, 8)})
+        _refused(binding.ERR_ARG, append, **{name: _as_table(on_ws((64,)), 8, 8)})
+    _refused(binding.ERR_ARG, rotary, outs=on_key(level - 1))
+    _refused(binding.ERR_ARG, rotary, keys=key_ws)
+    _refused(binding.ERR_ARG, rotary, cts=[C(on_ws((2, level, P.N)))])
+    _refused(binding.ERR_ARG, rotary, outs=[C(on_ws((2, level - 1, P.N)))])
+    _refused(binding.ERR_ARG, append, out_k=on_key(level - 1))
+    _refused(binding.ERR_ARG, append, pv=on_key(level - 1))
+    _refused(binding.ERR_ARG, append, keys=key_ws)
+    _refused(binding.ERR_ARG, append, k=[C(on_ws((2, level, P.N)))])
+    _refused(binding.ERR_ARG, append, v=[C(on_ws((2, level, P.N)))])
+    _refused(binding.ERR_ARG, append, pk=[C(on_ws((2, level - 1, P.N)))])
+    # score maps
+    y, z = _dev_cts(_residues(P, 5, level, 2)), _dev_cts(_residues(P, 6, level, 2))
+    outs = [C(torch.empty((2, level - 1, P.N), dtype=torch.uint64, device="cuda")) for _ in y]
+    w = torch.ones(2, dtype=torch.float64, device="cuda")
+    mask = lambda **kw: ctx.attention_mask(kw.get("x", y), 8, 2, 4, outs=kw.get("outs", outs), ws=ws)  # noqa: E731
+    diff = lambda **kw: ctx.attention_difference(kw.get("x", y), kw.get("y", z), kw.get("w", w), 8, 2, 4, outs=kw.get("outs", outs), ws=ws)  # noqa: E731
+    for f in (mask, diff):
+        _refused(binding.ERR_ARG, f, x=[y[0], C(on_ws((2, level, P.N)))])
+        _refused(binding.ERR_ARG, f, outs=[outs[0], C(on_ws((2, level - 1, P.N)))])
+    _refused(binding.ERR_ARG, diff, y=[C(on_ws((2, level, P.N))), z[1]])
+    _refused(binding.ERR_ARG, diff, w=_as_table(outs[1].data, 1, 2).view(-1))
+    _refused(binding.ERR_ARG, diff, w=_as_table(on_ws((64,)), 1, 2).view(-1))
+    assert binding.kernel_launches() == launches
+    rotary(), append(), mask(), diff()                       # and none of it with buffers of their own

@@ -82,19 +82,21 @@ uint32_t log2_ceil(uint32_t x) { uint32_t d = 0; while ((1ull << d) < x) d++; re
 
 extern "C" int32_t ckks_attention_rotations(const ckks_ctx *c, const ckks_attn_desc *d, int64_t *rots, uint32_t cap) {
     if (!c) return CKKS_ERR_ARG;
-    AttnPlan p;
-    int rc = make_attn_plan(c, d, p);
-    if (rc) return rc;
-    uint32_t k = 0;
-    for (int64_t r : p.tok) { if (rots && k < cap) rots[k] = r; k++; }
-    for (int64_t r : p.lad) { if (rots && k < cap) rots[k] = r; k++; }
-    for (int64_t r : p.neg) { if (rots && k < cap) rots[k] = r; k++; }
-    return (int32_t)k;
+    return guarded([&]() -> int32_t {
+        AttnPlan p;
+        int rc = make_attn_plan(c, d, p);
+        if (rc) return rc;
+        uint32_t k = 0;
+        for (int64_t r : p.tok) { if (rots && k < cap) rots[k] = r; k++; }
+        for (int64_t r : p.lad) { if (rots && k < cap) rots[k] = r; k++; }
+        for (int64_t r : p.neg) { if (rots && k < cap) rots[k] = r; k++; }
+        return (int32_t)k;
+    });
 }
 
 // ---- scores -------------------------------------------------------------------------------------------------------
 // workspace: [pass groups][dim] rotated key operands, the scratch of the steps
-extern "C" size_t ckks_attention_scores_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level, uint32_t dim) {
+static size_t scores_need(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level, uint32_t dim) {
     AttnPlan p;
     if (!c || !dim || level < 2 || level > c->L || make_attn_plan(c, d, p)) return 0;
     // the split holds Gb - 1 rotated key sets, G / Gb - 1 rotated query sets and the rescaled sums of one giant step
@@ -102,6 +104,9 @@ extern "C" size_t ckks_attention_scores_workspace_bytes(const ckks_ctx *c, const
         return (size_t)(p.Gb + p.G / p.Gb - 2) * dim * ct_bytes(c, level) + p.Gb * ct_bytes(c, level) +
                scratch_bytes(c, level, dim, std::max(p.Gb, p.G / p.Gb) - 1, p.G);
     return (size_t)(p.G - 1) * dim * ct_bytes(c, level) + scratch_bytes(c, level, dim, p.G - 1, p.G);
+}
+extern "C" size_t ckks_attention_scores_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level, uint32_t dim) {
+    return guarded_size([&] { return scores_need(c, d, level, dim); });
 }
 
 // scores with the groups split into Gb baby and G / Gb giant steps
@@ -149,9 +154,8 @@ static int scores_split(ckks_ctx *c, const AttnPlan &p, const ckks_ct *q, const 
     return rc;
 }
 
-extern "C" int32_t ckks_attention_scores(ckks_ctx *c, const ckks_attn_desc *d, const ckks_ct *q, const ckks_ct *k, uint32_t dim,
-                                         const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *scores, void *ws, size_t ws_bytes,
-                                         void *stream) {
+static int scores_run(ckks_ctx *c, const ckks_attn_desc *d, const ckks_ct *q, const ckks_ct *k, uint32_t dim, const ckks_evk *rlk, const ckks_evk *keys,
+                      uint32_t nkeys, ckks_ct *scores, void *ws, size_t ws_bytes, void *stream) {
     if (!c || !scores) return CKKS_ERR_ARG;
     AttnPlan p;
     int rc = make_attn_plan(c, d, p);
@@ -167,7 +171,7 @@ extern "C" int32_t ckks_attention_scores(ckks_ctx *c, const ckks_attn_desc *d, c
     for (uint32_t g = 0; g < p.G; g++)
         if (!scores[g].data) return CKKS_ERR_ARG;
     if (p.Gb > 1) {
-        if (!ws || ws_bytes < ckks_attention_scores_workspace_bytes(c, d, level, dim)) return CKKS_ERR_WORKSPACE;
+        if (!ws || ws_bytes < scores_need(c, d, level, dim)) return CKKS_ERR_WORKSPACE;
         return scores_split(c, p, q, k, dim, level, rlk, keys, nkeys, scores, ws, (cudaStream_t)stream);
     }
     // As many groups per pass as the workspace holds.  A workspace too small for one next to the steps' full scratch takes one
@@ -206,6 +210,12 @@ extern "C" int32_t ckks_attention_scores(ckks_ctx *c, const ckks_attn_desc *d, c
         scores[g].level = level - 1; scores[g].ncomp = 2; scores[g].scale = q[0].scale * k[0].scale / (double)c->mod[level - 1];
     }
     return rc;
+}
+extern "C" int32_t ckks_attention_scores(ckks_ctx *c, const ckks_attn_desc *d, const ckks_ct *q, const ckks_ct *k, uint32_t dim,
+                                         const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *scores, void *ws, size_t ws_bytes,
+                                         void *stream) {
+    if (!c) return CKKS_ERR_ARG;
+    return guarded(c, [&] { return scores_run(c, d, q, k, dim, rlk, keys, nkeys, scores, ws, ws_bytes, stream); });
 }
 
 // ---- masks of score rows, differences of score maps --------------------------------------------------------------------
@@ -269,10 +279,13 @@ static bool results_apart(const ckks_ctx *c, uint32_t level, const ckks_ct *cons
     return buffers.apart();
 }
 
-extern "C" size_t ckks_attention_mask_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
+static size_t mask_need(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
     AttnPlan p;
     if (!c || level < 2 || level > c->L || make_attn_plan(c, d, p)) return 0;
     return plain_steps_bytes(c, level, std::min(p.G, KS_MULTI), std::min(p.G, KS_MULTI));
+}
+extern "C" size_t ckks_attention_mask_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
+    return guarded_size([&] { return mask_need(c, d, level); });
 }
 
 extern "C" int32_t ckks_attention_mask(ckks_ctx *c, const ckks_attn_desc *d, const ckks_attn_mask *m, const ckks_ct *in, ckks_ct *out, void *ws, size_t ws_bytes,
@@ -288,7 +301,7 @@ extern "C" int32_t ckks_attention_mask(ckks_ctx *c, const ckks_attn_desc *d, con
         if (level < 2) return CKKS_ERR_LEVEL;
         for (uint32_t g = 0; g < p.G; g++)
             if (!out[g].data) return CKKS_ERR_ARG;
-        const size_t need = ckks_attention_mask_workspace_bytes(c, d, level);
+        const size_t need = mask_need(c, d, level);
         if (!ws || ws_bytes < need) return CKKS_ERR_WORKSPACE;
         if (!results_apart(c, level, &in, 1, nullptr, 0, out, p.G, ws, need)) return CKKS_ERR_ARG;
         std::vector<const u64 *> vi;
@@ -302,10 +315,13 @@ extern "C" int32_t ckks_attention_mask(ckks_ctx *c, const ckks_attn_desc *d, con
     });
 }
 
-extern "C" size_t ckks_attention_difference_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
+static size_t difference_need(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
     AttnPlan p;
     if (!c || level < 2 || level > c->L || make_attn_plan(c, d, p)) return 0;
     return plain_steps_bytes(c, level, std::min(p.G, KS_MULTI), 1);
+}
+extern "C" size_t ckks_attention_difference_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
+    return guarded_size([&] { return difference_need(c, d, level); });
 }
 
 extern "C" int32_t ckks_attention_difference(ckks_ctx *c, const ckks_attn_desc *d, const ckks_ct *x, const ckks_ct *y, const double *weights, ckks_ct *out, void *ws,
@@ -323,7 +339,7 @@ extern "C" int32_t ckks_attention_difference(ckks_ctx *c, const ckks_attn_desc *
             if (!scales_agree(x[g].scale, y[g].scale)) return CKKS_ERR_SCALE;
         }
         const ckks_ct *ins[2] = {x, y};
-        const size_t need = ckks_attention_difference_workspace_bytes(c, d, level);
+        const size_t need = difference_need(c, d, level);
         if (!ws || ws_bytes < need) return CKKS_ERR_WORKSPACE;
         if (!results_apart(c, level, ins, 2, weights, p.H, out, p.G, ws, need)) return CKKS_ERR_ARG;
         DeviceGuard guard(c->device);
@@ -346,10 +362,13 @@ static size_t rows_scratch(const ckks_ctx *c, const AttnPlan &p, const ckks_soft
 }
 
 // workspace: the groups' running ciphertexts u_g and their other copy, the row sums (twice) and lambda, the scratch of the steps
-extern "C" size_t ckks_softmax_rows_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, uint32_t level) {
+static size_t rows_need(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, uint32_t level) {
     AttnPlan p;
     if (!c || level < 1 || level > c->L || !rows_desc_ok(s) || make_attn_plan(c, d, p)) return 0;
     return (size_t)(2 * p.G + 3) * ct_bytes(c, level) + rows_scratch(c, p, s, level);
+}
+extern "C" size_t ckks_softmax_rows_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, uint32_t level) {
+    return guarded_size([&] { return rows_need(c, d, s, level); });
 }
 
 // Levels that the Softmax takes from its input, and its levels, scales and constants.  The groups' scales agree within 2^-30 and need not be
@@ -469,7 +488,7 @@ static int softmax_rows(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax
         if (s->rounds && (!keys || !find_key(c, keys, nkeys, r))) return CKKS_ERR_NO_KEY;
     for (uint32_t g = 0; g < p.G; g++)
         if (!out[g].data) return CKKS_ERR_ARG;
-    if (!ws || ws_bytes < ckks_softmax_rows_workspace_bytes(c, d, s, level)) return CKKS_ERR_WORKSPACE;
+    if (!ws || ws_bytes < rows_need(c, d, s, level)) return CKKS_ERR_WORKSPACE;
     RowsPlan plan;
     std::vector<double> scales;
     for (uint32_t g = 0; g < p.G; g++) scales.push_back(in[g].scale);
@@ -484,7 +503,8 @@ static int softmax_rows(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax
 
 extern "C" int32_t ckks_softmax_rows(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_ct *in, const ckks_evk *rlk,
                                      const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
-    return softmax_rows(c, d, s, nullptr, in, rlk, keys, nkeys, out, ws, ws_bytes, stream);
+    if (!c) return CKKS_ERR_ARG;
+    return guarded(c, [&] { return softmax_rows(c, d, s, nullptr, in, rlk, keys, nkeys, out, ws, ws_bytes, stream); });
 }
 extern "C" int32_t ckks_softmax_rows_masked(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_attn_mask *mask, const ckks_ct *in,
                                             const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
@@ -499,15 +519,17 @@ static size_t values_scratch(const ckks_ctx *c, uint32_t level, uint32_t nrot) {
     return std::max(scratch_bytes(c, level, VAL_CHUNK, nrot, VAL_CHUNK), align256(VAL_CHUNK * ks_workspace_limbs(c, level - 1) * c->N * sizeof(u64)));
 }
 // workspace: a chunk's rotated value operands, its outputs' other copy for the ladder, the scratch of the steps
-extern "C" size_t ckks_attention_values_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
+static size_t values_need(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
     AttnPlan p;
     if (!c || level < 2 || level > c->L || make_attn_plan(c, d, p)) return 0;
     return VAL_CHUNK * ((size_t)(p.G - 1) * ct_bytes(c, level) + ct_bytes(c, level - 1)) + values_scratch(c, level, p.G - 1);
 }
+extern "C" size_t ckks_attention_values_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, uint32_t level) {
+    return guarded_size([&] { return values_need(c, d, level); });
+}
 
-extern "C" int32_t ckks_attention_values(ckks_ctx *c, const ckks_attn_desc *d, const ckks_ct *probs, const ckks_ct *v, uint32_t dim_v,
-                                         const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes,
-                                         void *stream) {
+static int values_run(ckks_ctx *c, const ckks_attn_desc *d, const ckks_ct *probs, const ckks_ct *v, uint32_t dim_v, const ckks_evk *rlk, const ckks_evk *keys,
+                      uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
     if (!c || !out) return CKKS_ERR_ARG;
     AttnPlan p;
     int rc = make_attn_plan(c, d, p);
@@ -522,7 +544,7 @@ extern "C" int32_t ckks_attention_values(ckks_ctx *c, const ckks_attn_desc *d, c
         if (!keys || !find_key(c, keys, nkeys, r)) return CKKS_ERR_NO_KEY;
     for (uint32_t dd = 0; dd < dim_v; dd++)
         if (!out[dd].data) return CKKS_ERR_ARG;
-    if (!ws || ws_bytes < ckks_attention_values_workspace_bytes(c, d, lp)) return CKKS_ERR_WORKSPACE;
+    if (!ws || ws_bytes < values_need(c, d, lp)) return CKKS_ERR_WORKSPACE;
     const size_t ctw = ct_bytes(c, lp) / sizeof(u64), ctw1 = ct_bytes(c, lp - 1) / sizeof(u64), N = c->N;
     u64 *vr = (u64 *)ws, *tmp = vr + VAL_CHUNK * (p.G - 1) * ctw;         // [G - 1][VAL_CHUNK] at lp, [VAL_CHUNK] at lp - 1
     void *sw = tmp + VAL_CHUNK * ctw1;
@@ -565,20 +587,27 @@ extern "C" int32_t ckks_attention_values(ckks_ctx *c, const ckks_attn_desc *d, c
     }
     return rc;
 }
+extern "C" int32_t ckks_attention_values(ckks_ctx *c, const ckks_attn_desc *d, const ckks_ct *probs, const ckks_ct *v, uint32_t dim_v,
+                                         const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes,
+                                         void *stream) {
+    if (!c) return CKKS_ERR_ARG;
+    return guarded(c, [&] { return values_run(c, d, probs, v, dim_v, rlk, keys, nkeys, out, ws, ws_bytes, stream); });
+}
 
 // ---- the three steps in a row -------------------------------------------------------------------------------------
-extern "C" size_t ckks_attention_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, uint32_t level, uint32_t dim) {
+static size_t attention_need(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, uint32_t level, uint32_t dim) {
     AttnPlan p;
     if (!c || level < 3 || level > c->L || !dim || !rows_desc_ok(s) || make_attn_plan(c, d, p)) return 0;
     const size_t held = (size_t)2 * p.G * ct_bytes(c, level - 1);        // scores and probabilities
-    const size_t steps = std::max({ckks_attention_scores_workspace_bytes(c, d, level, dim), ckks_softmax_rows_workspace_bytes(c, d, s, level - 1),
-                                   ckks_attention_values_workspace_bytes(c, d, level - 1)});
+    const size_t steps = std::max({scores_need(c, d, level, dim), rows_need(c, d, s, level - 1), values_need(c, d, level - 1)});
     return held + steps;
 }
+extern "C" size_t ckks_attention_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, uint32_t level, uint32_t dim) {
+    return guarded_size([&] { return attention_need(c, d, s, level, dim); });
+}
 
-extern "C" int32_t ckks_attention(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_ct *q, const ckks_ct *k, uint32_t dim,
-                                  const ckks_ct *v, uint32_t dim_v, const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out,
-                                  void *ws, size_t ws_bytes, void *stream) {
+static int attention_run(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_ct *q, const ckks_ct *k, uint32_t dim, const ckks_ct *v,
+                         uint32_t dim_v, const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
     if (!c || !q || !dim) return CKKS_ERR_ARG;
     AttnPlan p;
     int rc = make_attn_plan(c, d, p);
@@ -586,7 +615,7 @@ extern "C" int32_t ckks_attention(ckks_ctx *c, const ckks_attn_desc *d, const ck
     if (!rows_desc_ok(s)) return CKKS_ERR_ARG;
     const uint32_t level = q[0].level;
     if (level < 3 || level > c->L) return CKKS_ERR_LEVEL;
-    const size_t need = ckks_attention_workspace_bytes(c, d, s, level, dim);
+    const size_t need = attention_need(c, d, s, level, dim);
     if (!ws || !need || ws_bytes < need) return CKKS_ERR_WORKSPACE;
     const size_t ctb = ct_bytes(c, level - 1);
     char *base = (char *)ws;
@@ -597,9 +626,15 @@ extern "C" int32_t ckks_attention(ckks_ctx *c, const ckks_attn_desc *d, const ck
     }
     void *sw = base + (size_t)2 * p.G * ctb;
     const size_t sw_bytes = ws_bytes - (size_t)2 * p.G * ctb;
-    if ((rc = ckks_attention_scores(c, d, q, k, dim, rlk, keys, nkeys, S.data(), sw, sw_bytes, stream))) return rc;
-    if ((rc = ckks_softmax_rows(c, d, s, S.data(), rlk, keys, nkeys, P.data(), sw, sw_bytes, stream))) return rc;
-    return ckks_attention_values(c, d, P.data(), v, dim_v, rlk, keys, nkeys, out, sw, sw_bytes, stream);
+    if ((rc = scores_run(c, d, q, k, dim, rlk, keys, nkeys, S.data(), sw, sw_bytes, stream))) return rc;
+    if ((rc = softmax_rows(c, d, s, nullptr, S.data(), rlk, keys, nkeys, P.data(), sw, sw_bytes, stream))) return rc;
+    return values_run(c, d, P.data(), v, dim_v, rlk, keys, nkeys, out, sw, sw_bytes, stream);
+}
+extern "C" int32_t ckks_attention(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_ct *q, const ckks_ct *k, uint32_t dim,
+                                  const ckks_ct *v, uint32_t dim_v, const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out,
+                                  void *ws, size_t ws_bytes, void *stream) {
+    if (!c) return CKKS_ERR_ARG;
+    return guarded(c, [&] { return attention_run(c, d, s, q, k, dim, v, dim_v, rlk, keys, nkeys, out, ws, ws_bytes, stream); });
 }
 
 // ---- masked attention, and the difference of two maps ------------------------------------------------------------------
@@ -609,8 +644,8 @@ static size_t maps_bytes(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_
     AttnPlan p;
     if (!c || level < 3 || level > c->L || !dim || !rows_desc_ok(s) || make_attn_plan(c, d, p)) return 0;
     return (size_t)(1 + maps) * p.G * ct_bytes(c, level - 1) +
-           std::max({ckks_attention_scores_workspace_bytes(c, d, level, dim), ckks_softmax_rows_workspace_bytes(c, d, s, level - 1),
-                     plain_steps_bytes(c, level - 1, std::min(p.G, KS_MULTI), 1), ckks_attention_values_workspace_bytes(c, d, level - 1)});
+           std::max({scores_need(c, d, level, dim), rows_need(c, d, s, level - 1), plain_steps_bytes(c, level - 1, std::min(p.G, KS_MULTI), 1),
+                     values_need(c, d, level - 1)});
 }
 static int attend(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_attn_mask *mask, const double *weights, uint32_t maps,
                   const ckks_ct *const *q, const ckks_ct *const *k, uint32_t dim, const ckks_ct *v, uint32_t dim_v, const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys,
@@ -660,7 +695,7 @@ static int attend(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc 
     DeviceGuard guard(c->device);
     for (uint32_t m = 0; m < maps; m++) {
         for (ckks_ct &x : S) x.level = level - 1;
-        if ((rc = ckks_attention_scores(c, d, q[m], k[m], dim, rlk, keys, nkeys, S.data(), sw, sw_bytes, stream))) return rc;
+        if ((rc = scores_run(c, d, q[m], k[m], dim, rlk, keys, nkeys, S.data(), sw, sw_bytes, stream))) return rc;
         rows_run(c, p, plan[m], mask, S.data(), (const u64 *)rlk->data, keys, nkeys, P[m].data(), sw, (cudaStream_t)stream);
     }
     const ckks_ct *probs = P[0].data();
@@ -669,11 +704,11 @@ static int attend(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc 
         for (uint32_t g = 0; g < p.G; g++) { S[g].level = plan[0].out_level - 1; S[g].ncomp = 2; S[g].scale = P[0][g].scale; }
         probs = S.data();
     }
-    return ckks_attention_values(c, d, probs, v, dim_v, rlk, keys, nkeys, out, sw, sw_bytes, stream);
+    return values_run(c, d, probs, v, dim_v, rlk, keys, nkeys, out, sw, sw_bytes, stream);
 }
 
 extern "C" size_t ckks_attention_masked_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, uint32_t level, uint32_t dim) {
-    return maps_bytes(c, d, s, level, dim, 1);
+    return guarded_size([&] { return maps_bytes(c, d, s, level, dim, 1); });
 }
 extern "C" int32_t ckks_attention_masked(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_attn_mask *mask, const ckks_ct *q, const ckks_ct *k,
                                          uint32_t dim, const ckks_ct *v, uint32_t dim_v, const ckks_evk *rlk, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out, void *ws,
@@ -682,7 +717,7 @@ extern "C" int32_t ckks_attention_masked(ckks_ctx *c, const ckks_attn_desc *d, c
     return guarded(c, [&] { return attend(c, d, s, mask, nullptr, 1, &q, &k, dim, v, dim_v, rlk, keys, nkeys, out, ws, ws_bytes, stream); });
 }
 extern "C" size_t ckks_attention_differential_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, uint32_t level, uint32_t dim) {
-    return maps_bytes(c, d, s, level, dim, 2);
+    return guarded_size([&] { return maps_bytes(c, d, s, level, dim, 2); });
 }
 extern "C" int32_t ckks_attention_differential(ckks_ctx *c, const ckks_attn_desc *d, const ckks_softmax_desc *s, const ckks_attn_mask *mask, const double *weights,
                                                const ckks_ct *q1, const ckks_ct *k1, const ckks_ct *q2, const ckks_ct *k2, uint32_t dim, const ckks_ct *v, uint32_t dim_v,
@@ -813,26 +848,31 @@ PackWs pack_layout(const ckks_ctx *c, const PackPlan &p, int kind, uint32_t leve
 
 extern "C" int32_t ckks_attention_pack_rotations(const ckks_ctx *c, const ckks_attn_desc *d, int32_t kind, uint32_t dim, int64_t *rots, uint32_t cap) {
     if (!c || kind < 0 || kind > 2) return CKKS_ERR_ARG;
-    AttnPlan ap;
-    PackPlan p;
-    int rc = make_pack_plan(c, d, dim, kind == 2, ap, p);
-    if (rc) return rc;
-    uint32_t k = 0;
-    list_rots(p.move, rots, cap, k);
-    if (kind == 0) list_rots(ap.lad, rots, cap, k);
-    if (kind == 1) { list_rots(p.dbl, rots, cap, k); list_rots(p.shA, rots, cap, k); list_rots(p.shB, rots, cap, k); }
-    return (int32_t)k;
+    return guarded([&]() -> int32_t {
+        AttnPlan ap;
+        PackPlan p;
+        int rc = make_pack_plan(c, d, dim, kind == 2, ap, p);
+        if (rc) return rc;
+        uint32_t k = 0;
+        list_rots(p.move, rots, cap, k);
+        if (kind == 0) list_rots(ap.lad, rots, cap, k);
+        if (kind == 1) { list_rots(p.dbl, rots, cap, k); list_rots(p.shA, rots, cap, k); list_rots(p.shB, rots, cap, k); }
+        return (int32_t)k;
+    });
 }
 
-extern "C" size_t ckks_attention_pack_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, int32_t kind, uint32_t level, uint32_t dim) {
+static size_t pack_need(const ckks_ctx *c, const ckks_attn_desc *d, int32_t kind, uint32_t level, uint32_t dim) {
     AttnPlan ap;
     PackPlan p;
     if (!c || kind < 0 || kind > 2 || level < 3 || level > c->L || make_pack_plan(c, d, dim, kind == 2, ap, p)) return 0;
     return pack_layout(c, p, kind, level, dim).bytes;
 }
+extern "C" size_t ckks_attention_pack_workspace_bytes(const ckks_ctx *c, const ckks_attn_desc *d, int32_t kind, uint32_t level, uint32_t dim) {
+    return guarded_size([&] { return pack_need(c, d, kind, level, dim); });
+}
 
-extern "C" int32_t ckks_attention_pack(ckks_ctx *c, const ckks_attn_desc *d, int32_t kind, const ckks_ct *in, uint32_t dim, const ckks_evk *keys,
-                                       uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
+static int pack_run(ckks_ctx *c, const ckks_attn_desc *d, int32_t kind, const ckks_ct *in, uint32_t dim, const ckks_evk *keys, uint32_t nkeys, ckks_ct *out,
+                    void *ws, size_t ws_bytes, void *stream) {
     if (!c || !out || kind < 0 || kind > 2) return CKKS_ERR_ARG;
     AttnPlan ap;
     PackPlan p;
@@ -952,4 +992,9 @@ extern "C" int32_t ckks_attention_pack(ckks_ctx *c, const ckks_attn_desc *d, int
     }
     lanes.join();
     return rc;
+}
+extern "C" int32_t ckks_attention_pack(ckks_ctx *c, const ckks_attn_desc *d, int32_t kind, const ckks_ct *in, uint32_t dim, const ckks_evk *keys,
+                                       uint32_t nkeys, ckks_ct *out, void *ws, size_t ws_bytes, void *stream) {
+    if (!c) return CKKS_ERR_ARG;
+    return guarded(c, [&] { return pack_run(c, d, kind, in, dim, keys, nkeys, out, ws, ws_bytes, stream); });
 }

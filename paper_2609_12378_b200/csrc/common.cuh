@@ -731,7 +731,8 @@ struct Buffers {
         return true;
     }
 };
-// An entry point's body: exceptions of host allocations end here
+// An entry point's body: exceptions of host allocations end here, those of a size with 0.  (Inside the library sizes come from functions that
+// throw: a 0 that stands for an exception is no size to compare a workspace with.)
 template <class F>
 inline int32_t guarded(ckks_ctx *c, F body) {
     try {
@@ -739,6 +740,22 @@ inline int32_t guarded(ckks_ctx *c, F body) {
     } catch (const std::exception &e) {
         try { c->cuda_error = e.what(); } catch (...) {}
         return CKKS_ERR_CUDA;
+    }
+}
+template <class F>
+inline int32_t guarded(F body) {
+    try {
+        return body();
+    } catch (const std::exception &) {
+        return CKKS_ERR_CUDA;
+    }
+}
+template <class F>
+inline size_t guarded_size(F body) {
+    try {
+        return body();
+    } catch (const std::exception &) {
+        return 0;
     }
 }
 inline bool scales_agree(double a, double b) { return fabs(a - b) <= ldexp(fmax(fabs(a), fabs(b)), -30); }

@@ -631,8 +631,22 @@ class Context:
             n = self._ws_bytes[key] = int(getattr(load(), size)(self._h, C.byref(make(*desc)), *args))
         return n
 
+    def _evk(self, key: SwitchKey, galois: int) -> CEvk:
+        t = _dev_u64(key.data)
+        self._here(t)
+        if t.numel() != 2 * self.dnum * (self.L + self.K) * self.N:
+            raise ValueError(f"expected a key of shape ({self.dnum}, 2, {self.L + self.K}, {self.N}), got {tuple(t.shape)}")
+        return CEvk(t.data_ptr(), galois)
+
     def _evks(self, keys):
-        return (CEvk * max(1, len(keys)))(*[CEvk(_dev_u64(x.data).data_ptr(), x.galois) for x in keys])
+        return (CEvk * max(1, len(keys)))(*[self._evk(x, x.galois) for x in keys])
+
+    def _scratch(self, ws: torch.Tensor):
+        """Address and bytes of a workspace."""
+        self._here(ws)
+        if not ws.is_contiguous():
+            raise ValueError("expected a contiguous workspace")
+        return ws.data_ptr(), ws.numel()
 
     @staticmethod
     def _mask(tokens, causal, key_begin, key_end, window, query_offset):
@@ -675,7 +689,7 @@ class Context:
         level = ia[0].level
         ws = self.workspace(self._need("ckks_attention_mask_workspace_bytes", shape, CAttnDesc, level)) if ws is None else ws
         outs, oa = self._results(outs, len(cts), max(level - 1, 1))
-        self._check(_lib.ckks_attention_mask(self._h, C.byref(d), C.byref(m), ia, oa, ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
+        self._check(_lib.ckks_attention_mask(self._h, C.byref(d), C.byref(m), ia, oa, *self._scratch(ws), _stream_ptr(stream)))
         for o, c in zip(outs, oa):
             o.scale = c.scale
         return outs
@@ -697,7 +711,7 @@ class Context:
         level = aa[0].level
         ws = self.workspace(self._need("ckks_attention_difference_workspace_bytes", shape, CAttnDesc, level)) if ws is None else ws
         outs, oa = self._results(outs, len(a), max(level - 1, 1))
-        self._check(_lib.ckks_attention_difference(self._h, C.byref(d), aa, ba, self._weights(weights, heads), oa, ws.data_ptr(), ws.numel(),
+        self._check(_lib.ckks_attention_difference(self._h, C.byref(d), aa, ba, self._weights(weights, heads), oa, *self._scratch(ws),
                                                    _stream_ptr(stream)))
         for o, c in zip(outs, oa):
             o.scale = c.scale
@@ -718,9 +732,9 @@ class Context:
             raise CkksError(ERR_ARG)
         ws = self.workspace(need)
         outs, oa = self._results(None, len(cts), level)
-        ck = CEvk(_dev_u64(rlk.data).data_ptr(), 0)
+        ck = self._evk(rlk, 0)
         self._check(_lib.ckks_softmax_rows_masked(self._h, C.byref(d), C.byref(sd), C.byref(m), ia, C.byref(ck), self._evks(keys), len(keys), oa,
-                                                  ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
+                                                  *self._scratch(ws), _stream_ptr(stream)))
         return [self._cut(o, c) for o, c in zip(outs, oa)]
 
     def attention_masked(self, q, k, v, shift, rounds, exp_coeffs, rsqrt_coeffs, rlk: SwitchKey, keys, tokens, heads, diag_block, token_inner: int = 1,
@@ -753,8 +767,8 @@ class Context:
         ws = self.workspace(need) if ws is None else ws
         qa, ka, va = [self._ct2s(x) for x in qs], [self._ct2s(x) for x in ks], self._ct2s(v)
         outs, oa = self._results(None, len(v), max(level - 1, 1))
-        ck = CEvk(_dev_u64(rlk.data).data_ptr(), 0)
-        tail = (dim, va, len(v), C.byref(ck), self._evks(keys), len(keys), oa, ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+        ck = self._evk(rlk, 0)
+        tail = (dim, va, len(v), C.byref(ck), self._evks(keys), len(keys), oa, *self._scratch(ws), _stream_ptr(stream))
         if weights is None:
             self._check(L.ckks_attention_masked(self._h, C.byref(d), C.byref(sd), C.byref(mask), qa[0], ka[0], *tail))
         else:
@@ -818,7 +832,7 @@ class Context:
         ws = self.workspace(self._need("ckks_rotary_workspace_bytes", shape, CRotaryDesc, level, n)) if ws is None else ws
         outs, oa = self._results(outs, n, max(level - 1, 1))
         self._check(_lib.ckks_rotary(self._h, C.byref(d), ia, (C.c_uint32 * n)(*rows), n, *self._table(cos, sin, d), self._evks(keys), len(keys), oa,
-                                     ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
+                                     *self._scratch(ws), _stream_ptr(stream)))
         for o, c in zip(outs, oa):
             o.scale = c.scale
         return outs
@@ -854,7 +868,7 @@ class Context:
         table = self._table(cos, sin, d) if cos is not None else (None, None, 0)
         (ik, pk, ok, _), (iv, pv, ov, _) = sides
         self._check(_lib.ckks_cache_append(self._h, C.byref(d), ik, iv, n, (C.c_uint32 * n)(*pages), (CCacheSpan * n)(*[CCacheSpan(*x) for x in spans]), pk, pv,
-                                           npages, *table, self._evks(keys), len(keys), ok, ov, ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
+                                           npages, *table, self._evks(keys), len(keys), ok, ov, *self._scratch(ws), _stream_ptr(stream)))
         for _, _, oa, out in sides:
             for p in pages if out is not None else ():
                 out[p].scale = oa[p].scale

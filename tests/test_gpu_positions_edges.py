@@ -159,3 +159,21 @@ def test_calls_on_tables_keys_weights_or_workspaces_in_their_results_place_are_r
     _refused(binding.ERR_ARG, diff, w=_as_table(on_ws((64,)), 1, 2).view(-1))
     assert binding.kernel_launches() == launches
     rotary(), append(), mask(), diff()                       # and none of it with buffers of their own
+
+
+def test_keys_of_another_level_and_workspaces_on_the_host_are_refused():
+    import torch
+    P, ctx = _ring(10)
+    a = (16, 4, 8)
+    x = _dev_cts(_residues(P, 1, 4, 1))
+    keys = _dev_keys(_keys(P, 2, P.oracle.rotary_rotations(*a, 16, False)))
+    cos, sin = ctx.rotary_table(16, 0, 8)
+    short = [binding.SwitchKey(k.data[:, :, :-1].contiguous(), k.galois) for k in keys]
+    launches = binding.kernel_launches()
+    with pytest.raises(ValueError):
+        ctx.rotary(x, [0], cos, sin, short, *a)
+    with pytest.raises(ValueError):
+        ctx.cache_append(x, None, [0], [(0, 1, 0)], _dev_cts(_residues(P, 3, 3, 1)), None, cos, sin, short, *a)
+    with pytest.raises(ValueError):
+        ctx.rotary(x, [0], cos, sin, keys, *a, ws=torch.empty(64 << 20, dtype=torch.uint8))
+    assert binding.kernel_launches() == launches

@@ -242,7 +242,7 @@ static void mask_groups(const ckks_ctx *c, const AttnPlan &p, const ckks_attn_ma
         a.pt = Ptrs(pts, ptw);
         a.pitch = a.level = level;
         launch_encode_slots(c, slots, nb, (double)c->mod[level - 1], rest, s);
-        launch_encode_coefs(c, rest, nb, 0, nb * level, plain_map(0, level), pts, s);
+        launch_encode_coefs(c, rest, nb, nb * level, plain_map(0, level), pts, s);
         launch_plain_rescale(c, a, (u64 *)rest, s, nb);
     }
 }
@@ -252,7 +252,7 @@ static void difference_groups(const ckks_ctx *c, const AttnPlan &p, const double
     u64 *pt = (u64 *)ws;
     void *rest = (char *)ws + align256((size_t)level * c->N * sizeof(u64));
     launch_encode_slots(c, SlotHeads{weights, log2_of(p.H), log2_of(p.Ti), log2_of(p.R)}, 1, (double)c->mod[level - 1], rest, s);
-    launch_encode_coefs(c, rest, 1, 0, level, plain_map(0, level), pt, s);
+    launch_encode_coefs(c, rest, 1, level, plain_map(0, level), pt, s);
     for (uint32_t g0 = 0; g0 < p.G; g0 += KS_MULTI) {
         const uint32_t nb = std::min(KS_MULTI, p.G - g0);
         PlainRescale a{};

@@ -665,11 +665,10 @@ struct SlotScores {
 // -weights[h] (device)
 struct SlotHeads { const double *weights; uint32_t heads, inner, copies /* logarithms */; };
 inline uint32_t log2_of(uint32_t pow2) { return (uint32_t)__builtin_ctz(pow2); }
-// The coefficients of `batch` <= 65535 plaintexts, formed in ws (encode_workspace_bytes), and the transform of the ones from `first` on to the limbs
-// of map (count limbs in all)
+// The coefficients of `batch` <= 65535 plaintexts, formed in ws (encode_workspace_bytes), and their transform to the limbs of map (`limbs` in all)
 template <class Slots>
 void launch_encode_slots(const ckks_ctx *c, const Slots &slots, uint32_t batch, double scale, void *ws, cudaStream_t s);
-void launch_encode_coefs(const ckks_ctx *c, const void *ws, uint32_t batch, uint32_t first, uint32_t limbs, const LimbMap &map, u64 *out, cudaStream_t s,
+void launch_encode_coefs(const ckks_ctx *c, const void *ws, uint32_t batch, uint32_t limbs, const LimbMap &map, u64 *out, cudaStream_t s,
                          bool sets = false);
 // Slot vectors of generalised diagonals, [count][n] fp64, for k = k0 .. k0+count-1 of one block pair, diagonal k pre-rotated by its
 // giant step's share k - k % B.

@@ -202,8 +202,8 @@ template void launch_encode_slots(const ckks_ctx *, const SlotTokens &, uint32_t
 template void launch_encode_slots(const ckks_ctx *, const SlotScores &, uint32_t, double, void *, cudaStream_t);
 template void launch_encode_slots(const ckks_ctx *, const SlotHeads &, uint32_t, double, void *, cudaStream_t);
 
-void launch_encode_coefs(const ckks_ctx *c, const void *ws, uint32_t batch, uint32_t first, uint32_t limbs, const LimbMap &map, u64 *out, cudaStream_t s, bool sets) {
-    const long long *coef = (const long long *)((const double2 *)ws + (size_t)batch * c->n) + (size_t)first * c->N;
+void launch_encode_coefs(const ckks_ctx *c, const void *ws, uint32_t batch, uint32_t limbs, const LimbMap &map, u64 *out, cudaStream_t s, bool sets) {
+    const long long *coef = (const long long *)((const double2 *)ws + (size_t)batch * c->n);
     NttPrologue pro{(const u64 *)coef, false, 0};
     pro.sets = sets;
     launch_ntt(c, out, limbs, map, false, s, nullptr, &pro);

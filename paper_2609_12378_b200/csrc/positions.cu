@@ -209,7 +209,7 @@ void rotate_items(ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, c
         }
         const uint32_t batch = ns * kinds;
         launch_encode_slots(c, slots, batch, scale, rest, side);
-        launch_encode_coefs(c, rest, batch, 0, batch * nt, set_map(level, p.nrot, kinds, c->K, c->L), pts, side, true);
+        launch_encode_coefs(c, rest, batch, batch * nt, set_map(level, p.nrot, kinds, c->K, c->L), pts, side, true);
         if (fork) lanes.mark(1);
         for (size_t i0 = 0; i0 < todo.size(); i0 += KS_MULTI) {
             const uint32_t nb = (uint32_t)std::min<size_t>(KS_MULTI, todo.size() - i0);
@@ -284,7 +284,7 @@ void append_items(ckks_ctx *c, uint32_t token_inner, const std::vector<Item> &it
             pr.in.p[i] = it.in; pr.acc.p[i] = it.acc; pr.out.p[i] = it.out;
         }
         launch_encode_slots(c, slots, nb, (double)c->mod[level - 1], rest, s);
-        launch_encode_coefs(c, rest, nb, 0, nb * level, plain_map(0, level), pts, s);
+        launch_encode_coefs(c, rest, nb, nb * level, plain_map(0, level), pts, s);
         launch_plain_rescale(c, pr, (u64 *)rest, s, nb);
     }
 }

@@ -177,3 +177,95 @@ def test_keys_of_another_level_and_workspaces_on_the_host_are_refused():
     with pytest.raises(ValueError):
         ctx.rotary(x, [0], cos, sin, keys, *a, ws=torch.empty(64 << 20, dtype=torch.uint8))
     assert binding.kernel_launches() == launches
+
+
+# ---- large calls and eight-byte alignment ------------------------------------------------------------------------------------------
+def _odd(arr):
+    """A ciphertext or key on the device eight bytes behind a sixteen-byte boundary."""
+    import torch
+    t = torch.empty(arr.size + 1, dtype=torch.int64, device="cuda")[1:].view(arr.shape)
+    t.copy_(torch.from_numpy(arr.view(np.int64)))
+    assert t.data_ptr() % 16 == 8
+    return t.view(torch.uint64)
+
+
+def _cts(x, odd):
+    return [binding.Ciphertext(_odd(c), SCALE) for c in x] if odd else _dev_cts(x)
+
+
+@pytest.mark.parametrize("odd", ["", "x", "y", "out", "x y out"])
+def test_masks_and_differences_of_many_limbs(odd):
+    """Sixteen groups at N = 2^13, level 7: more rows than are taken by a warp each."""
+    import torch
+    from tests.gpu_util import host
+    P, ctx = _ring(13)
+    o, level, shape = P.oracle, 7, (128, 4, 8)
+    desc = AttnDesc(*shape)
+    assert (P.N >> 10) * 2 * desc.groups() * (level - 1) > 6 * 148
+    x, y = _residues(P, 51, level, 16), _residues(P, 52, level, 16)
+    dx, dy = _cts(x, "x" in odd), _cts(y, "y" in odd)
+    fresh = lambda: _cts(np.zeros((16, 2, level - 1, P.N), dtype=np.uint64), "out" in odd)  # noqa: E731
+    kw = dict(causal=True, key_begin=2, key_end=120, window=70)
+    got, want = ctx.attention_mask(dx, *shape, outs=fresh(), **kw), o.attention_mask(desc, x, **kw)
+    for g in range(16):
+        assert np.array_equal(host(got[g].data), want[g]), g
+    w = np.array([0.5, -1.25, 0.0, 0.7])
+    got, want = ctx.attention_difference(dx, dy, torch.from_numpy(w).cuda(), *shape, outs=fresh()), o.attention_difference(desc, x, y, w)
+    for g in range(16):
+        assert np.array_equal(host(got[g].data), want[g]), g
+
+
+@pytest.mark.parametrize("log_n,level,shape,n", [(12, 6, (32, 4, 16), 3), (13, 7, (64, 8, 8), 16)])
+@pytest.mark.parametrize("odd", ["", "in", "page", "out", "key", "in page out key"])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_append_of_unaligned_buffers(log_n, level, shape, n, odd, in_place):
+    """Whole pages and parts of pages, rotated keys, values and keys without positions; the larger case has more rows than are taken by a warp each."""
+    import torch
+    from tests.gpu_util import host
+    P, ctx = _ring(log_n)
+    o, inner, half = P.oracle, shape[2], shape[0] // 2
+    keys = _keys(P, 61, o.rotary_rotations(*shape, shape[0], False))
+    dk = [binding.SwitchKey(_odd(k), g) for g, k in keys.items()] if "key" in odd else _dev_keys(keys)
+    xk, xv = _residues(P, 62, level, n), _residues(P, 63, level, n)
+    pk, pv = _residues(P, 64, level - 1, n), _residues(P, 65, level - 1, n)
+    spans = [(0, inner, 0)] + [(i % 5, inner - i % 3 - 1, i) for i in range(1, n)]
+    a = np.random.default_rng(66).uniform(-4, 4, (n + inner, half))
+    cos, sin = np.cos(a), np.sin(a)
+    dc, ds = torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda()
+    pages = list(range(n))
+    for table, parts in (((dc, ds), spans), ((dc, ds), [(1, inner, 0)] + spans[1:]), ((None, None), spans)):
+        dxk, dxv = _cts(xk, "in" in odd), _cts(xv, "in" in odd)
+        dpk, dpv = _cts(pk, "page" in odd), _cts(pv, "page" in odd)
+        fresh = lambda: _cts(np.zeros_like(pk), "out" in odd)  # noqa: E731
+        ok, ov = ctx.cache_append(dxk, dxv, pages, parts, dpk, dpv, *table, dk, *shape, out_k=None if in_place else fresh(), out_v=None if in_place else fresh())
+        for i, (b, e, r) in enumerate(parts):
+            want = o.append_keys(pk[i], xk[i], cos, sin, keys, *shape, shape[0], False, b, e, r) if table[0] is not None else o.append_values(pk[i], xk[i], inner, b, e)
+            assert np.array_equal(host(ok[i].data), want), i
+            assert np.array_equal(host(ov[i].data), o.append_values(pv[i], xv[i], inner, b, e)), i
+
+
+# ---- options on the ring that they change ------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("layout,rot", [("half", 128), ("interleaved", 40)])
+def test_rotation_with_options_that_change_its_kernels(layout, rot):
+    """N = 2^16: conversions on the tensor cores, a share of the plain transforms on the integer pipe, and both, which leave the fused row kernel."""
+    import torch
+    from tests.gpu_util import host
+    P, ctx = _ring(16)
+    o, a, il = P.oracle, (128, 32, 8), layout == "interleaved"
+    keys = _keys(P, 71, o.rotary_rotations(*a, rot, il))
+    x, dk = _residues(P, 72, 3, 2), _dev_keys(keys)
+    ang = np.random.default_rng(73).uniform(-4, 4, (16, rot // 2))
+    cos, sin = np.cos(ang), np.sin(ang)
+    dc, ds = torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda()
+    want, d = o.rotary(x, [0, 5], cos, sin, keys, *a, rot, il), _dev_cts(x)
+    both = {binding.OPT_CONV_KERNEL: binding.CONV_TENSOR, binding.OPT_NTT_FP_SHARE: 3}
+    for options in (both, {binding.OPT_CONV_KERNEL: binding.CONV_TENSOR}, {binding.OPT_NTT_FP_SHARE: 3}, {binding.OPT_CONV_KERNEL: binding.CONV_TENSOR, binding.OPT_NTT_FP_SHARE: 0}):
+        old = {k: ctx.get_option(k) for k in options}
+        try:
+            for k, v in options.items():
+                ctx.set_option(k, v)
+            out = ctx.rotary(d, [0, 5], dc, ds, dk, *a, rot_dim=rot, layout=layout)
+        finally:
+            for k, v in old.items():
+                ctx.set_option(k, v)
+        assert all(np.array_equal(host(out[i].data), want[i]) for i in range(2)), options

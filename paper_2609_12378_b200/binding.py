@@ -641,12 +641,12 @@ class Context:
     def _evks(self, keys):
         return (CEvk * max(1, len(keys)))(*[self._evk(x, x.galois) for x in keys])
 
-    def _scratch(self, ws: torch.Tensor):
-        """Address and bytes of a workspace."""
+    def _given(self, ws: torch.Tensor) -> torch.Tensor:
+        """A workspace of the caller's."""
         self._here(ws)
         if not ws.is_contiguous():
             raise ValueError("expected a contiguous workspace")
-        return ws.data_ptr(), ws.numel()
+        return ws
 
     @staticmethod
     def _mask(tokens, causal, key_begin, key_end, window, query_offset):
@@ -687,9 +687,9 @@ class Context:
             raise ValueError("expected one ciphertext per group of diag_block diagonals")
         ia = self._ct2s(cts)
         level = ia[0].level
-        ws = self.workspace(self._need("ckks_attention_mask_workspace_bytes", shape, CAttnDesc, level)) if ws is None else ws
+        ws = self.workspace(self._need("ckks_attention_mask_workspace_bytes", shape, CAttnDesc, level)) if ws is None else self._given(ws)
         outs, oa = self._results(outs, len(cts), max(level - 1, 1))
-        self._check(_lib.ckks_attention_mask(self._h, C.byref(d), C.byref(m), ia, oa, *self._scratch(ws), _stream_ptr(stream)))
+        self._check(_lib.ckks_attention_mask(self._h, C.byref(d), C.byref(m), ia, oa, ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
         for o, c in zip(outs, oa):
             o.scale = c.scale
         return outs
@@ -709,9 +709,9 @@ class Context:
             raise ValueError("expected one ciphertext per group of diag_block diagonals")
         aa, ba = self._ct2s(a), self._ct2s(b)
         level = aa[0].level
-        ws = self.workspace(self._need("ckks_attention_difference_workspace_bytes", shape, CAttnDesc, level)) if ws is None else ws
+        ws = self.workspace(self._need("ckks_attention_difference_workspace_bytes", shape, CAttnDesc, level)) if ws is None else self._given(ws)
         outs, oa = self._results(outs, len(a), max(level - 1, 1))
-        self._check(_lib.ckks_attention_difference(self._h, C.byref(d), aa, ba, self._weights(weights, heads), oa, *self._scratch(ws),
+        self._check(_lib.ckks_attention_difference(self._h, C.byref(d), aa, ba, self._weights(weights, heads), oa, ws.data_ptr(), ws.numel(),
                                                    _stream_ptr(stream)))
         for o, c in zip(outs, oa):
             o.scale = c.scale
@@ -734,7 +734,7 @@ class Context:
         outs, oa = self._results(None, len(cts), level)
         ck = self._evk(rlk, 0)
         self._check(_lib.ckks_softmax_rows_masked(self._h, C.byref(d), C.byref(sd), C.byref(m), ia, C.byref(ck), self._evks(keys), len(keys), oa,
-                                                  *self._scratch(ws), _stream_ptr(stream)))
+                                                  ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
         return [self._cut(o, c) for o, c in zip(outs, oa)]
 
     def attention_masked(self, q, k, v, shift, rounds, exp_coeffs, rsqrt_coeffs, rlk: SwitchKey, keys, tokens, heads, diag_block, token_inner: int = 1,
@@ -764,11 +764,11 @@ class Context:
         need = int(size(self._h, C.byref(d), C.byref(sd), level, dim))
         if need == 0:
             raise CkksError(ERR_ARG)
-        ws = self.workspace(need) if ws is None else ws
+        ws = self.workspace(need) if ws is None else self._given(ws)
         qa, ka, va = [self._ct2s(x) for x in qs], [self._ct2s(x) for x in ks], self._ct2s(v)
         outs, oa = self._results(None, len(v), max(level - 1, 1))
         ck = self._evk(rlk, 0)
-        tail = (dim, va, len(v), C.byref(ck), self._evks(keys), len(keys), oa, *self._scratch(ws), _stream_ptr(stream))
+        tail = (dim, va, len(v), C.byref(ck), self._evks(keys), len(keys), oa, ws.data_ptr(), ws.numel(), _stream_ptr(stream))
         if weights is None:
             self._check(L.ckks_attention_masked(self._h, C.byref(d), C.byref(sd), C.byref(mask), qa[0], ka[0], *tail))
         else:
@@ -829,10 +829,10 @@ class Context:
         if len(rows) != n:
             raise ValueError("expected one table row per ciphertext")
         ia = self._ct2s(cts)
-        ws = self.workspace(self._need("ckks_rotary_workspace_bytes", shape, CRotaryDesc, level, n)) if ws is None else ws
+        ws = self.workspace(self._need("ckks_rotary_workspace_bytes", shape, CRotaryDesc, level, n)) if ws is None else self._given(ws)
         outs, oa = self._results(outs, n, max(level - 1, 1))
         self._check(_lib.ckks_rotary(self._h, C.byref(d), ia, (C.c_uint32 * n)(*rows), n, *self._table(cos, sin, d), self._evks(keys), len(keys), oa,
-                                     *self._scratch(ws), _stream_ptr(stream)))
+                                     ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
         for o, c in zip(outs, oa):
             o.scale = c.scale
         return outs
@@ -863,12 +863,11 @@ class Context:
             sides.append((self._ct2s(cts), cp, co, out))
         if npages is None:
             raise CkksError(ERR_ARG)
-        if ws is None:
-            ws = self.workspace(self._need("ckks_cache_append_workspace_bytes", shape, CRotaryDesc, level, n))
+        ws = self.workspace(self._need("ckks_cache_append_workspace_bytes", shape, CRotaryDesc, level, n)) if ws is None else self._given(ws)
         table = self._table(cos, sin, d) if cos is not None else (None, None, 0)
         (ik, pk, ok, _), (iv, pv, ov, _) = sides
         self._check(_lib.ckks_cache_append(self._h, C.byref(d), ik, iv, n, (C.c_uint32 * n)(*pages), (CCacheSpan * n)(*[CCacheSpan(*x) for x in spans]), pk, pv,
-                                           npages, *table, self._evks(keys), len(keys), ok, ov, *self._scratch(ws), _stream_ptr(stream)))
+                                           npages, *table, self._evks(keys), len(keys), ok, ov, ws.data_ptr(), ws.numel(), _stream_ptr(stream)))
         for _, _, oa, out in sides:
             for p in pages if out is not None else ():
                 out[p].scale = oa[p].scale

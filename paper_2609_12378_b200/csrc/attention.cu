@@ -270,6 +270,7 @@ static bool results_apart(const ckks_ctx *c, uint32_t level, const ckks_ct *cons
                           const void *ws, size_t ws_bytes) {
     const size_t bi = (size_t)2 * level * c->N * sizeof(u64), bo = (size_t)2 * (level - 1) * c->N * sizeof(u64);
     Buffers buffers;
+    buffers.all.reserve((nin + 1) * G + 2);
     if (weights) buffers.read(weights, heads * sizeof(double));
     buffers.write(ws, ws_bytes);
     for (uint32_t g = 0; g < G; g++) {
@@ -301,7 +302,8 @@ extern "C" int32_t ckks_attention_mask(ckks_ctx *c, const ckks_attn_desc *d, con
         if (level < 2) return CKKS_ERR_LEVEL;
         for (uint32_t g = 0; g < p.G; g++)
             if (!out[g].data) return CKKS_ERR_ARG;
-        const size_t need = mask_need(c, d, level);
+        const uint32_t side = std::min(p.G, KS_MULTI);
+        const size_t need = plain_steps_bytes(c, level, side, side);
         if (!ws || ws_bytes < need) return CKKS_ERR_WORKSPACE;
         if (!results_apart(c, level, &in, 1, nullptr, 0, out, p.G, ws, need)) return CKKS_ERR_ARG;
         std::vector<const u64 *> vi;
@@ -339,7 +341,7 @@ extern "C" int32_t ckks_attention_difference(ckks_ctx *c, const ckks_attn_desc *
             if (!scales_agree(x[g].scale, y[g].scale)) return CKKS_ERR_SCALE;
         }
         const ckks_ct *ins[2] = {x, y};
-        const size_t need = difference_need(c, d, level);
+        const size_t need = plain_steps_bytes(c, level, std::min(p.G, KS_MULTI), 1);
         if (!ws || ws_bytes < need) return CKKS_ERR_WORKSPACE;
         if (!results_apart(c, level, ins, 2, weights, p.H, out, p.G, ws, need)) return CKKS_ERR_ARG;
         DeviceGuard guard(c->device);

@@ -74,15 +74,16 @@ def test_keys_of_another_shape_or_device_are_refused():
 
 def test_workspaces_of_another_device_are_refused():
     ctx = _context()
-    assert ctx._scratch(_Tensor((512,), dtype=torch.uint8)) == (4096, 512)
+    ws = _Tensor((512,), dtype=torch.uint8)
+    assert ctx._given(ws) is ws
     for kw in (dict(device=1), dict(device=-1), dict(contiguous=False)):
         with pytest.raises(ValueError):
-            ctx._scratch(_Tensor((512,), dtype=torch.uint8, **kw))
+            ctx._given(_Tensor((512,), dtype=torch.uint8, **kw))
 
 
 def test_every_call_of_positions_and_maps_checks_its_keys_and_workspace():
     """The methods that hand keys and workspaces on do so through the checks above."""
     for name in ("attention_mask", "attention_difference", "softmax_rows_masked", "_attend", "rotary", "cache_append"):
         source = inspect.getsource(getattr(binding.Context, name))
-        assert "self._scratch(ws)" in source and "ws.data_ptr()" not in source, name
+        assert ("ws: torch.Tensor" not in source and name != "_attend") or "if ws is None else self._given(ws)" in source, name
         assert "rlk.data" not in source and ("keys" not in source or "self._evks(keys)" in source), name

@@ -283,8 +283,8 @@ __global__ void __launch_bounds__(32 * MID_ROWS, 6) mid_rows_pos(DevTables c, co
 
 // Five to eight digits: a CTA per row, a warp per digit, then the row's pairs of both components over all threads, because one warp would
 // transform the digits one after the other (one ciphertext at N = 2^13, six digits: 47 us for the call, 41 with launches of their own for the
-// transforms and positions_inner, 37 so; sixteen 116 against 119).  With three digits it is slower from the first ciphertext on at N = 2^16 (180 -> 212
-// us for a token's append) and little faster at N = 2^14 (86 -> 84).
+// transforms and positions_inner, 37 so; wide_rows in positions.cu says up to where).  With three digits it is slower from the first ciphertext on at
+// N = 2^16 (180 -> 212 us for a token's append) and little faster at N = 2^14 (86 -> 84).
 template <uint32_t BETA>
 __global__ void __launch_bounds__(32 * BETA) mid_rows_pos_wide(DevTables c, const __grid_constant__ PosArgs a) {
     constexpr uint32_t THREADS = 32 * BETA, ITEMS = (256 + THREADS - 1) / THREADS;
@@ -369,7 +369,10 @@ void launch_mid_rows_pos(const ckks_ctx *c, const PosArgs &a, uint32_t beta, cud
         return;
     }
     PosArgs b = a;
-    b.share = a.nb % 4 == 0 || a.nb > 12 ? 2 : a.nb % 2 == 0 || a.nb > 4 ? 1 : 0;        // few idle warps: groups that the entries fill, or many groups
+    // entries of a row in a CTA: few idle warps, so groups that they fill, or many groups.  Rotation at N = 2^16, level 24, in ones / twos / fours, us: one
+    // ciphertext 188 / 206 / 241, two 292 / 291 / 321, three 416 / 416 / 417, four 544 / 531 / 531, five 638 / 640 / 660, six 747 / 738 / 756, eight
+    // 954 / 944 / 939, twelve 1391 / 1376 / 1367, thirteen 1510 / 1510 / 1508, sixteen 1808 / 1787 / 1789
+    b.share = a.nb % 4 == 0 || a.nb > 12 ? 2 : a.nb % 2 == 0 || a.nb > 4 ? 1 : 0;
     const uint32_t e = 1u << b.share;
     launch((a.nrot > 1 ? many : one)[beta - 1], dim3((c->N >> 8) / (MID_ROWS >> b.share), (a.nb + e - 1) / e, a.level + c->K), 32 * MID_ROWS, 0, s, c->dev, b);
 }

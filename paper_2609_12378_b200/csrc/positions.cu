@@ -140,9 +140,22 @@ const ckks_evk *find_key(const ckks_ctx *c, const ckks_evk *keys, uint32_t nkeys
 }
 
 // Calls of a few ciphertexts on large rings, whose launches leave most of the GPU idle, run what does not depend on each other side by side: the
-// plaintexts' encoding next to the extension of the digits, the values next to the keys (one token's append at N = 2^16, level 18, 213 -> 180 us).
-// Smaller rings' short calls are bound by the host, to which the fork's events cost more than it gains.
+// plaintexts' encoding next to the extension of the digits, the values next to the keys.  An append on one stream / on two, us: N = 2^16, level 18,
+// one ciphertext 215 / 187, two 355 / 327, four 657 / 634, eight 1192 / 1181, sixteen 2304 / 2310; N = 2^15, level 10, one 91 / 81, four 191 / 169,
+// eight 336 / 308, sixteen 621 / 589; a rotation gains at most 10 (166 / 156).  On smaller rings the fork's events cost the host of a short call
+// what the GPU gains, or more: N = 2^13, level 6, one 59.1 / 61.1, two 71.4 / 73.0, eight 109 / 112; N = 2^14, one 58.2 / 60.5, two 63.7 / 63.7.
+// (The same calls from a graph, 48 / 33, 53 / 39, 96 / 82 and 55 / 40, 63 / 55, and from four on at N = 2^14, 84 / 80, would gain; the rule looks
+// at the ring and the number alone.)
 bool side_by_side(const ckks_ctx *c, uint32_t n) { return c->log_n >= 15 && n <= (4u << (16 - c->log_n)); }
+
+// mid_rows_pos_wide takes the rows of five to eight digits while its CTAs, one per row, are few: 25 per SM with one rotation, 10 with two, for which
+// it transforms the digits twice and plain transforms before positions_inner once.  Call, us, with launches apart / with it: six digits at N = 2^13, one
+// rotation, one ciphertext 42 / 38, eight 68 / 63, sixteen 106 / 104; at N = 2^14 eight 112 / 110, sixteen 187 / 191; two rotations at N = 2^13, one 44 / 40,
+// six 70 / 67, eight 77 / 78, sixteen 122 / 131; eight digits at N = 2^13, two rotations, three 62.5 / 60.6, five 81 / 81, sixteen 176 / 193.  From
+// N = 2^15 on launches apart fill the GPU from the first ciphertext: five digits, one rotation 65 / 69, two rotations 81 / 92, sixteen 588 / 704.
+bool wide_rows(const ckks_ctx *c, uint32_t level, uint32_t nrot, uint32_t nb) {
+    return c->log_n <= 14 && (uint64_t)(c->N >> 8) * nb * (level + c->K) <= (nrot == 1 ? 25 : 10) * (uint64_t)c->sms;
+}
 
 // Workspace of a pass over up to `m` sets of positions and `m` ciphertexts side by side: plaintexts, then the encoder's scratch, whose
 // place the key switches take over (side by side: behind it), and after them the values'
@@ -228,8 +241,7 @@ void rotate_items(ckks_ctx *c, const ckks_rotary_desc *d, const RotaryPlan &p, c
                 const ckks_evk *k = find_key(c, keys, nkeys, p.rots[r]);
                 a.evk[r] = (const u64 *)k->data; a.galois[r] = k->galois;
             }
-            // five and more digits of many ciphertexts and two rotations are transformed once for both (N = 2^13, six digits, sixteen: 153 -> 144 us)
-            w.mid = ks_mid(c, level, w, c1, a.evk, p.nrot, p.nrot == 1 || nb < 8 ? POS_BETA : IP_FUSED_BETA) && aligned16(a.c) && aligned16(pts);
+            w.mid = ks_mid(c, level, w, c1, a.evk, p.nrot, wide_rows(c, level, p.nrot, nb) ? POS_BETA : IP_FUSED_BETA) && aligned16(a.c) && aligned16(pts);
             auto append_values = [&]() {
                 PlainRescale v{};
                 v.in.n = v.pt.n = v.acc.n = v.out.n = nb;

@@ -269,3 +269,23 @@ def test_rotation_with_options_that_change_its_kernels(layout, rot):
             for k, v in old.items():
                 ctx.set_option(k, v)
         assert all(np.array_equal(host(out[i].data), want[i]) for i in range(2)), options
+
+
+# ---- five to eight digits: the row kernel and the launches apart ----------------------------------------------------------------------
+@pytest.mark.parametrize("ring,level,shape,n", [((12, 6, 1, 6), 6, (16, 4, 32), 13), ((12, 6, 1, 6), 6, (16, 4, 32), 18), ((13, 8, 1, 8), 8, (16, 4, 32), 5),
+                                                ((13, 8, 1, 8), 7, (16, 4, 32), 16), ((14, 6, 1, 6), 6, (32, 8, 16), 1), ((14, 6, 1, 6), 5, (32, 8, 16), 16),
+                                                ((15, 10, 2, 5), 10, (64, 16, 16), 1), ((15, 10, 2, 5), 9, (64, 16, 16), 3)])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rotation_of_many_digits_on_both_sides_of_its_rule(ring, level, shape, n, layout):
+    import torch
+    from tests.gpu_util import context, host
+    P, ctx = params(*ring), context(*ring)
+    o, il, rows = P.oracle, layout == "interleaved", [i % 3 for i in range(n)]
+    keys = _keys(P, 81, o.rotary_rotations(*shape, shape[0], il))
+    x, dk = _residues(P, 82, level, n), _dev_keys(keys)
+    a = np.random.default_rng(83).uniform(-4, 4, (2 + shape[2], shape[0] // 2))
+    cos, sin = np.cos(a), np.sin(a)
+    out = ctx.rotary(_dev_cts(x), rows, torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda(), dk, *shape, layout=layout)
+    want = o.rotary(x, rows, cos, sin, keys, *shape, shape[0], il)
+    for i in range(n):
+        assert np.array_equal(host(out[i].data), want[i]), i

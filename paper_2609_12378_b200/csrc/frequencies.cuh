@@ -155,7 +155,9 @@ inline void rotary_frequencies(const ckks_rotary_scaling &f, double few, double 
             if (num.h <= 0.0) {
                 a = mul(a, inv_factor);
             } else if (rest.h > 0.0) {
-                a = add(mul(mul(num, inv_den), a), mul(mul(rest, inv_den), mul(a, inv_factor)));
+                // (one over a bound's distance next to the smallest double is no number)
+                const Pair kept = isfinite(inv_den.h) ? mul(num, inv_den) : number(num.h / den.h), gone = isfinite(inv_den.h) ? mul(rest, inv_den) : number(rest.h / den.h);
+                a = add(mul(kept, a), mul(gone, mul(a, inv_factor)));
             }
         }
         a = mul(a, inv_pi);

@@ -84,3 +84,11 @@ def test_a_far_position_is_as_exact_as_a_near_one(lib):
         hi, lo = lib(*a)
         for j, w in enumerate(angles(*a)):
             assert abs((Decimal(hi[j]) + Decimal(lo[j])) * PI - w) * 2 ** 50 < Decimal(2) ** -49, (kind, j)
+
+
+def test_bounds_next_to_the_smallest_double(lib):
+    """Numbers there have few bits (the distance of the bounds 45, so that a part is off by 2^-44), and one over their distance is infinite."""
+    hi, lo = lib(8, 10000.0, "bands", 4.0, 1.2e-309, 1e-310, 3e-310)
+    want = angles(8, 10000.0, "bands", 4.0, 1.2e-309, 1e-310, 3e-310)
+    for j, w in enumerate(want):
+        assert abs((Decimal(hi[j]) + Decimal(lo[j])) * PI - w) <= w * Decimal(2) ** -40, j

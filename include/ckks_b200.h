@@ -418,7 +418,8 @@ size_t ckks_attention_differential_workspace_bytes(const ckks_ctx *ctx, const ck
  *              divided by factor, between them blended linearly in the number of turns;
  *       RAMP:  the same blended linearly in j, from the (rounded down) pair that turns turns_many (0: 32) times to the (rounded up) one that
  *              turns turns_few (0: 1) times.
- *     Angles are formed and reduced as sums of two doubles: far positions are as exact as near ones (up to 2^50).  rot_dim even, <= 256.
+ *     Frequencies and angles are formed and reduced as sums of two doubles: at every position up to 2^50 a value is within 2^-49 of its own,
+ *     times the magnitude.  rot_dim even, <= 256; cos and sin apart.
  *   ckks_rotary: the position rotation of n shard ciphertexts, slot t of in[i] at row rows[i] + t * row_step of the tables (row_step 0: all slots
  *     hold one token's copies).  The first rot_dim channels of every head are rotated in pairs: layout HALF pairs d with d + rot_dim / 2,
  *     INTERLEAVED 2 j with 2 j + 1; channel d of pair j:
@@ -438,7 +439,8 @@ size_t ckks_attention_differential_workspace_bytes(const ckks_ctx *ctx, const ck
  *     host arrays of npages descriptors, of which the named pages are read and written, out_k[p] may be page_k[p] (in place).  Pages at one level l,
  *     inputs at one level above it per side, of which l + 1 limbs are read; the scales of inputs and pages agree within 2^-30.  A page may be named
  *     once.  Keys and values of a page written by ckks_cache_append go to ckks_attention_pack as they are, with ckks_attn_mask's key_end at
- *     the number of tokens.
+ *     the number of tokens.  The attention over them is that of a map: as many queries as keys, heads * tokens <= n, so a longer cache is a map per
+ *     n / heads tokens, and a single generated query costs the whole map (there is no call for one query alone).
  * Written buffers (the workspace is one) may not overlap each other or anything that is read (tables and keys too), but for a page in place.
  * Errors: ARG (also a table row past table_rows, a page number past npages, an empty span), LEVEL, SCALE, NO_KEY, WORKSPACE, UNSUPPORTED (dim *
  * heads * token_inner does not divide n, rot_dim odd or above dim).  Tables are read when the kernels run; values beyond the encoder's range set ckks_encode_range_flag. */

@@ -1,6 +1,7 @@
 // Frequencies of position tables: the angle per position of every pair over pi, as an unevaluated sum of two doubles.  A position of up to 2^50
-// multiplies a frequency's error, so the power, the scalings and the division by pi are all carried to at least 100 bits: w within 2^-100 of
-// itself and the far angle within 2^-50 of its own value.  Host code in integers and doubles, 64 pairs in about as long as 64 calls of pow.
+// multiplies a frequency's error, so the power, the scalings and the division by pi are carried to at least 99 bits (the most that was seen is
+// 2^-103.7): no angle up to there is off by more than 2^-52 for it.  Host code in integers and doubles: 64 pairs in 1.0 us, as long as 64 calls of
+// pow, and in 1.7 to 2.4 us where pairs are blended.
 #pragma once
 #include <math.h>
 #include <stdint.h>

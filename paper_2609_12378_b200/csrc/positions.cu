@@ -36,7 +36,8 @@ __device__ __forceinline__ double2 unit(double pos, double w_hi, double w_lo) {
 }
 // cos, sin [count][half] of position first + row, a CTA per R^2 rows and 32 columns: R + R units per column from the functions, the others
 // as products e^(i w (base + offset)), four operations where the function takes tens.  Their error is that of two units, of the
-// magnitude's product and of their own: below 7 * 2^-52 times the magnitude, and 2^-52 from the frequency at position 2^50.  Bound by its stores from R = 16 on: 131072 positions of 64 pairs, 134 MB, in 25.6 us (5.2 TB/s; 121 us with every value from the function).
+// magnitude's product and of their own: below 7 * 2^-52 times the magnitude, and 2^-52 from the frequency at position 2^50.  Bound by its
+// stores from R = 16 on: 131072 positions of 64 pairs, 134 MB, in 24.9 us (5.4 TB/s; 121 us with every value from the function).
 template <uint32_t R>
 __global__ void __launch_bounds__(THREADS) rotary_table_kernel(const __grid_constant__ Turns w, uint64_t first, uint64_t count, uint32_t half, double magnitude,
                                                              double *cosv, double *sinv) {
